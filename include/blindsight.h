@@ -410,6 +410,150 @@ int bs_aggregate_layer(const uint8_t *head_types, int32_t n_prompts, int32_t n_q
  */
 double bs_alpha_layer(double alpha_first, double alpha_last, int32_t layer_idx, int32_t num_layers);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Around the KV cache: rotary positions, a cache in pages, attention of one new token per sequence over it, and eviction
+ * from it.  With bs_attn_prefill before them these are a model's attention from the prompt to the last token of the answer.
+ * A generated token is text, and text tokens see every earlier token under every head class (paper Sec. 3.2), so the
+ * classes play no part here.  (The paper keeps the whole cache; bs_cache_evict is for those who cannot.)
+ *
+ * These calls keep nothing: no state of the library, no allocation, no wait.  They enqueue kernels on `stream` (NULL = default
+ * stream) and can be captured into a HIP graph; what changes from token to token (lengths, slots, positions, page
+ * tables) lies on the device.  Workspaces are the caller's: a call owns its workspace until its kernels are done, so calls that may
+ * overlap, and graphs that may be replayed at the same time, need one each.  All pointers are device pointers of the
+ * current HIP device unless they say host, and `stream` is one of its streams.  Threads may call at the same time.
+ * Errors of all of them: BS_EINVAL (null pointers, sizes or strides that cannot be, a workspace that is too small),
+ * BS_EUNSUPPORTED (dtype, head_dim, page size or alignment that the kernels do not implement), BS_EHIP.  Nothing is launched on error.
+ */
+
+/* Some heads of some tokens: element c of head h of token t at data[h * head_stride + t * token_stride + c], strides in
+ * elements, >= 0.  [n_heads][n_tokens][head_dim] and [n_tokens][n_heads][head_dim] are both of this kind. */
+typedef struct { void *data; int64_t head_stride, token_stride; int32_t n_heads; } bs_heads;
+
+#define BS_ROPE_HALF        0   /* channel i turns with channel i + rotary_dim / 2        */
+#define BS_ROPE_INTERLEAVED 1   /* channel 2 i turns with channel 2 i + 1                 */
+
+#define BS_ROPE_PLAIN  0   /* f_i = base^(-2 i / rotary_dim), in radians per position                                        */
+#define BS_ROPE_LINEAR 1   /* f_i / factor                                                                                   */
+#define BS_ROPE_BASE   2   /* f_i of the base times factor^(rotary_dim / (rotary_dim - 2)): the slowest pair turns 1 / factor as fast */
+#define BS_ROPE_PARTS  3   /* f_i (g + (1 - g) / factor), g = (n_i - slow) / (fast - slow) held within [0, 1], n_i the turns that pair i
+                              makes over original_len positions: fast pairs stay as they are, slow ones are interpolated       */
+
+#define BS_ROPE_MAX_PAIRS 128
+#define BS_ROPE_MAX_AXES  4
+
+/* Rotary positions: pair i of a head is turned by the angle position[axis[i]] * freq[i] and multiplied by `magnitude`; channels
+ * from rotary_dim on are left as they are.  Plain data on the host, copied by every call: bs_rope_init fills it in, and a
+ * caller may change freq, axis or magnitude afterwards. */
+typedef struct {
+    int32_t rotary_dim;                  /* even, 2 .. 2 * BS_ROPE_MAX_PAIRS                  */
+    int32_t layout;                      /* BS_ROPE_HALF or BS_ROPE_INTERLEAVED               */
+    int32_t n_axes;                      /* axes of a position, 1 .. BS_ROPE_MAX_AXES         */
+    float magnitude;
+    double freq[BS_ROPE_MAX_PAIRS];
+    uint8_t axis[BS_ROPE_MAX_PAIRS];     /* which axis of the position turns a pair           */
+} bs_rope;
+
+/*
+ * Fill in *rope (host only).  original_len, fast and slow are looked at for BS_ROPE_PARTS only, factor for all but
+ * BS_ROPE_PLAIN.  sections (host, n_axes values >= 0 that add up to rotary_dim / 2; NULL for one axis): the first
+ * sections[0] pairs follow axis 0, the next ones axis 1, and so on (multimodal models: time, height, width).
+ * Errors: BS_EINVAL; *rope is untouched then.
+ */
+int bs_rope_init(bs_rope *rope, int32_t rotary_dim, int32_t layout, double base, int32_t scaling, double factor,
+                 int32_t original_len, double fast, double slow, double magnitude, const int32_t *sections, int32_t n_axes);
+
+#define BS_ROPE_INVERSE 1u   /* turn backwards: the gradient of the rotation (same magnitude) */
+
+/*
+ * Apply rotary positions to n_tensors (1 or 2: q and k of a layer) sets of heads of the same tokens.
+ *   x, y       host, [n_tensors]; y[i] as many heads as x[i].  y may be x itself (same data and strides), else they do
+ *              not overlap
+ *   head_dim   even, rotary_dim <= head_dim <= 2 * BS_ROPE_MAX_PAIRS
+ *   positions  device, row a = axis a, axis_stride elements apart: positions[a * axis_stride + t], any 32-bit value
+ *   flags      0 or BS_ROPE_INVERSE
+ * The angle is formed and reduced in 64 bits, so far positions turn as exactly as near ones; the product is fp32, rounded
+ * once.  Any alignment and stride; 16-byte loads are used where pointers, strides and sizes allow them.  n_tokens may be 0.
+ */
+int bs_rope_apply(const bs_rope *rope, const bs_heads *x, const bs_heads *y, int32_t n_tensors, int32_t dtype, int32_t n_tokens,
+                  int32_t head_dim, const int32_t *positions, int64_t axis_stride, uint32_t flags, void *stream);
+
+/* A KV cache in pages.  Slot j of sequence s and KV head h lies in page p = page_table[s * max_pages + j / page_size] at
+ * k[p * page_stride + h * head_stride + (j % page_size) * slot_stride], head_dim contiguous elements, and likewise in v; strides in
+ * elements, so that [page][head][slot][d] and [page][slot][head][d] both fit.  A page number outside [0, n_pages) means that these
+ * slots have no page: they are not written, and nobody sees them.  k and v 16-byte aligned, strides multiples of 16 bytes;
+ * head_dim a multiple of 8 up to 256 (bs_attn_decode: 64 or 128), page_size a multiple of 16. */
+typedef struct {
+    void *k, *v;
+    const int32_t *page_table;                       /* device [n_seqs][max_pages]                     */
+    int64_t page_stride, head_stride, slot_stride;
+    int32_t dtype;                                   /* BS_BF16 or BS_F32                              */
+    int32_t n_kv_heads, head_dim, page_size, n_pages;
+    int32_t n_seqs, max_pages;
+} bs_cache;
+
+/* What is known of every slot besides K and V, per sequence and KV head; row s * n_kv_heads + h, row_stride >= max_pages *
+ * page_size elements apart.  weights: the attention that the slot has received; order: the running number of its token in the
+ * sequence (once slots were evicted, slots no longer lie in that order). */
+typedef struct { float *weights; int32_t *order; int64_t row_stride; } bs_slots;
+
+/*
+ * Write new tokens into the cache: K rotated if `rope` is not NULL, V as it is; and rotate q of the same step along.
+ *   k, v         n_kv_heads heads of n_tokens tokens in the cache's dtype; any strides
+ *   token_seq    device [n_tokens]: the sequence of each token; NULL: token t belongs to sequence t
+ *   token_slot   device [n_tokens]: the slot it goes to.  A token whose sequence or slot is out of range (a padded batch: -1), or
+ *                whose slot has no page, is not written.  No two tokens may name one slot.
+ *   rope, positions, axis_stride   as for bs_rope_apply; NULL: K and q are not rotated
+ *   q, q_out     as x and y of bs_rope_apply; both NULL: no q.  With q, rope may not be NULL.
+ *   slots        NULL, or what is set for every slot written (either pointer may be NULL): weights 0, order token_order[t] (device
+ *                [n_tokens]; NULL: the slot's number)
+ * The lengths of the sequences are the caller's to count.
+ */
+int bs_cache_append(const bs_cache *cache, const bs_heads *k, const bs_heads *v, int32_t n_tokens, const int32_t *token_seq,
+                    const int32_t *token_slot, const bs_rope *rope, const int32_t *positions, int64_t axis_stride, const bs_heads *q,
+                    const bs_heads *q_out, const bs_slots *slots, const int32_t *token_order, void *stream);
+
+/*
+ * Attention of one new token per sequence over the cache, its own slot included:
+ *   out[s, h, :] = sum_j softmax_j( scale * <q[s, h], K[s, h / G, j]> ) * V[s, h / G, j, :],  G = n_q_heads / n_kv_heads,
+ * over the slots j < lens[s], with window > 0 only those with lens[s] - j <= window; zeros where there is none.
+ *   q, out       n_q_heads heads of n_seqs tokens (token s = sequence s) in the cache's dtype, 16-byte aligned, strides
+ *                multiples of 16 bytes; n_q_heads a multiple of n_kv_heads; out does not overlap q
+ *   lens         device [n_seqs]; held within [0, max_pages * page_size]
+ *   slots, slots_out   NULL, or (both) weights_out[j] = weights[j] + the sum over the group's G heads of the probability of slot j,
+ *                for j < lens[s]; other entries are not touched.  slots_out may be slots, else they do not overlap.  order is
+ *                not looked at.  Not together with a window (BS_EUNSUPPORTED).
+ *   workspace    at least bs_attn_decode_workspace bytes, 16-byte aligned
+ * Slots that are not seen may hold anything, infinities and NaN too; a seen one with such a value makes the rows that see it
+ * not finite.  bf16: probabilities are rounded to bf16 before P V, as in the prefill; sums, maxima and weights are fp32.
+ * Same inputs, same bits: nothing depends on the order in which workgroups finish.
+ */
+int bs_attn_decode(const bs_cache *cache, const bs_heads *q, const bs_heads *out, const int32_t *lens, int32_t window, float scale,
+                   const bs_slots *slots, const bs_slots *slots_out, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace of bs_attn_decode for this cache and head count, with weights or without; a negative error code for
+ * arguments that the call would refuse.  Depends on the sizes in *cache, not on lengths; on the current device's number of compute units. */
+int64_t bs_attn_decode_workspace(const bs_cache *cache, int32_t n_q_heads, int32_t with_weights);
+
+/*
+ * Cut the cache back to `keep` slots per sequence and KV head, where it holds more.  Kept are the slots whose order is below
+ * keep_first or above (the largest order of the row) - keep_last, and of the others those with the largest weights; of equal
+ * weights the lower slot; a NaN counts as the smallest.  keep >= 1, keep_first + keep_last <= keep.  (Where orders repeat, so
+ * that the first two are more than `keep`: the lowest of these slots.)
+ * Kept slots at or behind `keep` move into the evicted slots before it, the first into the first, and so on, K, V, weight and order
+ * alike; all other slots stay where they are.  (So as few as can be move: a row cut back from 4160 slots to 4096 moves at most 64.  Keys
+ * carry their positions, attention does not mind the order.)  A slot without a page moves its weight and order alone.
+ *   lens, lens_out     device [n_seqs]: slots in use (held within [0, max_pages * page_size]), and min(lens, keep); may be the same
+ *   slots, slots_out   weights and order before and after; entries from lens_out on are not touched; may be the same, else they do not
+ *                      overlap
+ *   workspace          at least bs_cache_evict_workspace bytes, 16-byte aligned
+ * Pages that are moved into must not be shared with other sequences.
+ */
+int bs_cache_evict(const bs_cache *cache, const int32_t *lens, int32_t *lens_out, int32_t keep, int32_t keep_first, int32_t keep_last,
+                   const bs_slots *slots, const bs_slots *slots_out, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace of bs_cache_evict for this cache; a negative error code for arguments that the call would refuse. */
+int64_t bs_cache_evict_workspace(const bs_cache *cache, int32_t keep);
+
 /* Static description of an error code (error behaviour of this boundary; no passage of the paper). */
 const char *bs_strerror(int code);
 

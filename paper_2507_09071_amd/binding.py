@@ -20,8 +20,9 @@ DENSE, SINK, INTRA, INTRA_SINK = 0, 1, 2, 3
 EXPORTS = ("bs_build_tilemap", "bs_build_tilemap_ex", "bs_build_tilemap_model", "bs_build_tilemap_suffix", "bs_tilemap_destroy", "bs_tilemap_dims", "bs_tilemap_row_order", "bs_tilemap_layout", "bs_tilemap_key_order", "bs_tilemap_tile_states", "bs_tilemap_walked",
            "bs_tilemap_stats", "bs_tilemap_pair_plan", "bs_tilemap_share_plan", "bs_tilemap_upload", "bs_tilemap_rebind", "bs_tilemap_prepare",
            "bs_attn_prefill", "bs_attn_prefill_ex", "bs_attn_prefill_static", "bs_static_scratch_bytes",
-           "bs_characterize_prompt", "bs_head_sq_error", "bs_aggregate_head_type", "bs_aggregate_layer", "bs_alpha_layer", "bs_strerror",
-           "bs_last_error")
+           "bs_characterize_prompt", "bs_head_sq_error", "bs_aggregate_head_type", "bs_aggregate_layer", "bs_alpha_layer",
+           "bs_rope_init", "bs_rope_apply", "bs_cache_append", "bs_attn_decode", "bs_attn_decode_workspace", "bs_cache_evict",
+           "bs_cache_evict_workspace", "bs_strerror", "bs_last_error")
 
 
 class BlindsightError(RuntimeError):
@@ -121,6 +122,21 @@ def load_library():
     lib.bs_aggregate_layer.restype = ctypes.c_int
     lib.bs_alpha_layer.argtypes = [f64, f64, i32, i32]
     lib.bs_alpha_layer.restype = ctypes.c_double
+    i64 = ctypes.c_int64
+    lib.bs_rope_init.argtypes = [vp, i32, i32, f64, i32, f64, i32, f64, f64, f64, vp, i32]
+    lib.bs_rope_init.restype = ctypes.c_int
+    lib.bs_rope_apply.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp, i64, ctypes.c_uint32, vp]
+    lib.bs_rope_apply.restype = ctypes.c_int
+    lib.bs_cache_append.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp]
+    lib.bs_cache_append.restype = ctypes.c_int
+    lib.bs_attn_decode.argtypes = [vp, vp, vp, vp, i32, ctypes.c_float, vp, vp, vp, i64, vp]
+    lib.bs_attn_decode.restype = ctypes.c_int
+    lib.bs_attn_decode_workspace.argtypes = [vp, i32, i32]
+    lib.bs_attn_decode_workspace.restype = i64
+    lib.bs_cache_evict.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp, i64, vp]
+    lib.bs_cache_evict.restype = ctypes.c_int
+    lib.bs_cache_evict_workspace.argtypes = [vp, i32]
+    lib.bs_cache_evict_workspace.restype = i64
     lib.bs_strerror.argtypes = [ctypes.c_int]
     lib.bs_strerror.restype = ctypes.c_char_p
     lib.bs_last_error.argtypes = []
@@ -391,3 +407,149 @@ def bs_aggregate_layer(head_types, gamma_d: float, gamma_s: float, gamma_i: floa
 def bs_alpha_layer(alpha_first: float, alpha_last: float, layer_idx: int, num_layers: int) -> float:
     """Linear alpha_layer schedule of the paper (fixed threshold when both ends are equal)."""
     return float(load_library().bs_alpha_layer(float(alpha_first), float(alpha_last), int(layer_idx), int(num_layers)))
+
+
+# ---------------------------------------------------------------------------------------- around the KV cache
+
+BS_ROPE_HALF, BS_ROPE_INTERLEAVED = 0, 1
+BS_ROPE_PLAIN, BS_ROPE_LINEAR, BS_ROPE_BASE, BS_ROPE_PARTS = 0, 1, 2, 3
+BS_ROPE_MAX_PAIRS = 128
+BS_ROPE_INVERSE = 1
+
+
+class Rope(ctypes.Structure):
+    """bs_rope: frequencies and layout of rotary positions, made by bs_rope_init."""
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("freq", ctypes.c_double * BS_ROPE_MAX_PAIRS), ("axis", ctypes.c_uint8 * BS_ROPE_MAX_PAIRS)]
+
+
+class Heads(ctypes.Structure):
+    """bs_heads: some heads of some tokens, at data + h * head_stride + t * token_stride (strides in elements)."""
+    _fields_ = [("data", ctypes.c_void_p), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("n_heads", ctypes.c_int32)]
+
+    @classmethod
+    def of(cls, x) -> "Heads":
+        """x: tensor viewed as [n_heads, n_tokens, head_dim], channels contiguous (or a Heads, returned as it is)."""
+        if isinstance(x, Heads):
+            return x
+        head, token, channel = x.stride()
+        if channel != 1:
+            raise ValueError("the channels of a head have to be contiguous")
+        return cls(x.data_ptr(), head, token, x.shape[0])
+
+
+class KVCache(ctypes.Structure):
+    """bs_cache: a KV cache in pages.  Holds addresses only; the caller keeps the arrays alive."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+    @classmethod
+    def of(cls, k, v, page_table, dtype: int) -> "KVCache":
+        """k, v: pools viewed as [n_pages, n_kv_heads, page_size, head_dim], alike in strides, channels contiguous;
+        page_table: contiguous int32 [n_seqs, max_pages]."""
+        if k.shape != v.shape or k.stride() != v.stride() or k.stride()[3] != 1:
+            raise ValueError("k and v have to be alike in shape and strides, with contiguous channels")
+        n_seqs, max_pages = page_table.shape
+        if not page_table.is_contiguous() or page_table.element_size() != 4:
+            raise ValueError("page_table has to be contiguous int32")
+        return cls(k.data_ptr(), v.data_ptr(), page_table.data_ptr(), *k.stride()[:3], int(dtype), k.shape[1], k.shape[3], k.shape[2],
+                   k.shape[0], n_seqs, max_pages)
+
+
+class CacheSlots(ctypes.Structure):
+    """bs_slots: the attention that every slot has received and the running number of its token."""
+    _fields_ = [("weights", ctypes.c_void_p), ("order", ctypes.c_void_p), ("row_stride", ctypes.c_int64)]
+
+    @classmethod
+    def of(cls, weights=None, order=None) -> "CacheSlots":
+        """weights: float32, order: int32, contiguous [n_seqs, n_kv_heads, slots] (either may be left out)."""
+        strides = {x.shape[-1] for x in (weights, order) if x is not None}
+        if len(strides) != 1 or not all(x is None or (x.is_contiguous() and x.element_size() == 4) for x in (weights, order)):
+            raise ValueError("weights and order have to be contiguous, of 32 bits and of one shape")
+        return cls(None if weights is None else weights.data_ptr(), None if order is None else order.data_ptr(), strides.pop())
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def _address(x):
+    return None if x is None else _ptr(x)
+
+
+def bs_rope_init(rotary_dim: int, layout: int = BS_ROPE_HALF, base: float = 1e4, scaling: int = BS_ROPE_PLAIN, factor: float = 1.0,
+                 original_len: int = 0, fast: float = 32.0, slow: float = 1.0, magnitude: float = 1.0, sections=None) -> Rope:
+    """sections: pairs that follow each axis of the positions (None: one axis)."""
+    rope = Rope()
+    so = None if sections is None else np.ascontiguousarray(sections, dtype=np.int32).reshape(-1)
+    rc = load_library().bs_rope_init(ctypes.byref(rope), int(rotary_dim), int(layout), float(base), int(scaling), float(factor), int(original_len),
+                                     float(fast), float(slow), float(magnitude), None if so is None else so.tobytes(), 1 if so is None else len(so))
+    _check(rc, "bs_rope_init")
+    return rope
+
+
+def bs_rope_apply(rope: Rope, xs, ys, dtype: int, n_tokens: int, head_dim: int, positions, axis_stride: int | None = None,
+                  inverse: bool = False, stream=None) -> None:
+    """xs, ys: one or two tensors [n_heads, n_tokens, head_dim] of any strides (or Heads), e.g. q and k; ys may be xs.  positions:
+    int32 [n_axes, n_tokens] on the device, rows axis_stride apart (n_tokens by default).  inverse: the gradient.  Enqueues only."""
+    n = len(xs)
+    if len(ys) != n:
+        raise ValueError("as many ys as xs")
+    arrays = Heads * n
+    rc = load_library().bs_rope_apply(ctypes.byref(rope), arrays(*map(Heads.of, xs)), arrays(*map(Heads.of, ys)), n, int(dtype), int(n_tokens),
+                                      int(head_dim), _ptr(positions), int(n_tokens if axis_stride is None else axis_stride),
+                                      BS_ROPE_INVERSE if inverse else 0, int(stream) if stream else None)
+    _check(rc, "bs_rope_apply")
+
+
+def bs_cache_append(cache: KVCache, k, v, n_tokens: int, token_seq, token_slot, rope: Rope | None = None, positions=None,
+                    axis_stride: int | None = None, q=None, q_out=None, slots: CacheSlots | None = None, token_order=None, stream=None) -> None:
+    """k, v, q, q_out: tensors [n_heads, n_tokens, head_dim] of any strides (or Heads); token_seq (None: token t is of sequence t),
+    token_slot, token_order (None: the slot's number): int32 on the device.  Enqueues only."""
+    rc = load_library().bs_cache_append(ctypes.byref(cache), ctypes.byref(Heads.of(k)), ctypes.byref(Heads.of(v)), int(n_tokens), _address(token_seq),
+                                        _ptr(token_slot), _ref(rope), _address(positions), int(n_tokens if axis_stride is None else axis_stride),
+                                        None if q is None else ctypes.byref(Heads.of(q)), None if q_out is None else ctypes.byref(Heads.of(q_out)),
+                                        _ref(slots), _address(token_order), int(stream) if stream else None)
+    _check(rc, "bs_cache_append")
+
+
+def _buffer(workspace):
+    """Address and bytes of a workspace: a tensor, or a pair of the two."""
+    if hasattr(workspace, "data_ptr"):
+        return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    address, n_bytes = workspace
+    return int(address), int(n_bytes)
+
+
+def bs_attn_decode(cache: KVCache, q, out, lens, scale: float, workspace, window: int = 0, slots: CacheSlots | None = None,
+                   slots_out: CacheSlots | None = None, stream=None) -> None:
+    """q, out: tensors [n_q_heads, n_seqs, head_dim] of any strides (or Heads); lens: int32 [n_seqs] on the device; workspace: a tensor, or
+    (address, bytes), of bs_attn_decode_workspace bytes.  slots, slots_out: add up the attention that every slot receives.  Enqueues only."""
+    rc = load_library().bs_attn_decode(ctypes.byref(cache), ctypes.byref(Heads.of(q)), ctypes.byref(Heads.of(out)), _ptr(lens), int(window), float(scale),
+                                       _ref(slots), _ref(slots_out), *_buffer(workspace), int(stream) if stream else None)
+    _check(rc, "bs_attn_decode")
+
+
+def bs_attn_decode_workspace(cache: KVCache, n_q_heads: int, with_weights: bool = False) -> int:
+    n = load_library().bs_attn_decode_workspace(ctypes.byref(cache), int(n_q_heads), int(bool(with_weights)))
+    if n < 0:
+        _check(int(n), "bs_attn_decode_workspace")
+    return int(n)
+
+
+def bs_cache_evict(cache: KVCache, lens, lens_out, keep: int, keep_first: int, keep_last: int, slots: CacheSlots, slots_out: CacheSlots, workspace,
+                   stream=None) -> None:
+    """lens, lens_out: int32 [n_seqs] on the device, may be the same, as slots and slots_out; workspace: a tensor, or (address, bytes), of
+    bs_cache_evict_workspace bytes.  Enqueues only."""
+    rc = load_library().bs_cache_evict(ctypes.byref(cache), _ptr(lens), _ptr(lens_out), int(keep), int(keep_first), int(keep_last), _ref(slots),
+                                       _ref(slots_out), *_buffer(workspace), int(stream) if stream else None)
+    _check(rc, "bs_cache_evict")
+
+
+def bs_cache_evict_workspace(cache: KVCache, keep: int) -> int:
+    n = load_library().bs_cache_evict_workspace(ctypes.byref(cache), int(keep))
+    if n < 0:
+        _check(int(n), "bs_cache_evict_workspace")
+    return int(n)

@@ -1,0 +1,158 @@
+"""What the calls around the KV cache refuse, before anything touches a GPU, and the frequencies of rotary positions."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+import paper_2507_09071_amd as bs
+from paper_2507_09071_amd import binding
+
+EINVAL, EUNSUPPORTED = -1, -2
+P = 4096   # an address, never used: the calls are refused
+
+
+def heads(n=8, data=P, head=128, token=1024):
+    return binding.Heads(data, head, token, n)
+
+
+def cache(**kw):
+    f = dict(k=P, v=P, page_table=P, page_stride=16 * 4 * 128, head_stride=16 * 128, slot_stride=128, dtype=bs.BS_BF16, n_kv_heads=4, head_dim=128,
+             page_size=16, n_pages=10, n_seqs=3, max_pages=7)
+    f.update(kw)
+    return bs.KVCache(**f)
+
+
+def ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+BAD_CACHES = [(dict(k=None), EINVAL), (dict(v=None), EINVAL), (dict(page_table=None), EINVAL), (dict(n_kv_heads=0), EINVAL), (dict(head_dim=-8), EINVAL),
+              (dict(page_size=0), EINVAL), (dict(n_pages=0), EINVAL), (dict(n_seqs=0), EINVAL), (dict(max_pages=-1), EINVAL), (dict(page_stride=-8), EINVAL),
+              (dict(slot_stride=2 ** 41), EINVAL), (dict(dtype=2), EUNSUPPORTED), (dict(head_dim=132), EUNSUPPORTED), (dict(head_dim=264), EUNSUPPORTED),
+              (dict(page_size=24), EUNSUPPORTED), (dict(page_size=8), EUNSUPPORTED), (dict(k=P + 8), EUNSUPPORTED), (dict(v=P + 2), EUNSUPPORTED),
+              (dict(slot_stride=132), EUNSUPPORTED), (dict(head_stride=4), EUNSUPPORTED), (dict(page_stride=12), EUNSUPPORTED),
+              (dict(max_pages=2 ** 27 + 2 ** 20), EUNSUPPORTED), (dict(slot_stride=2 ** 27), EUNSUPPORTED), (dict(n_seqs=2 ** 30), EUNSUPPORTED)]
+
+
+@pytest.mark.parametrize("bad,code", BAD_CACHES)
+def test_caches(bad, code):
+    lib, c, h, s = binding.load_library(), cache(**bad), heads(4), bs.CacheSlots(P, P, 1 << 36)
+    assert lib.bs_cache_append(ref(c), ref(h), ref(h), 3, None, P, None, None, 0, None, None, None, None, None) == code
+    assert lib.bs_cache_evict(ref(c), P, P, 5, 0, 0, ref(s), ref(s), P, 1 << 40, None) == code
+    assert lib.bs_cache_evict_workspace(ref(c), 5) == code
+    assert lib.bs_attn_decode(ref(c), ref(heads()), ref(heads()), P, 0, 0.1, None, None, P, 1 << 40, None) == code
+    assert lib.bs_attn_decode_workspace(ref(c), 8, 0) == code
+
+
+def test_no_cache():
+    lib, h = binding.load_library(), heads(4)
+    assert lib.bs_cache_append(None, ref(h), ref(h), 3, None, P, None, None, 0, None, None, None, None, None) == EINVAL
+    assert lib.bs_cache_evict_workspace(None, 5) == EINVAL and lib.bs_attn_decode_workspace(None, 8, 0) == EINVAL
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(q=None), EINVAL), (dict(out=None), EINVAL), (dict(q=heads(data=None)), EINVAL), (dict(q=heads(6), out=heads(6)), EINVAL), (dict(out=heads(4)), EINVAL),
+    (dict(q=heads(0), out=heads(0)), EINVAL), (dict(lens=None), EINVAL), (dict(window=-1), EINVAL), (dict(scale=0.0), EINVAL), (dict(scale=math.nan), EINVAL),
+    (dict(scale=math.inf), EINVAL), (dict(scale=-1.0), EINVAL), (dict(slots=None), EINVAL), (dict(slots_out=None), EINVAL), (dict(workspace=None), EINVAL),
+    (dict(workspace=P + 8), EINVAL), (dict(n_bytes=-1), EINVAL), (dict(slots=bs.CacheSlots(None, P, 112)), EINVAL), (dict(slots=bs.CacheSlots(P, P, 111)), EINVAL),
+    (dict(slots=bs.CacheSlots(P, P, 120)), EINVAL), (dict(slots_out=bs.CacheSlots(P + 2, P, 112)), EINVAL), (dict(window=5), EUNSUPPORTED),
+    (dict(q=heads(data=P + 8)), EUNSUPPORTED), (dict(out=heads(head=132)), EUNSUPPORTED), (dict(q=heads(token=-8)), EINVAL), (dict(cache=cache(head_dim=256)), EUNSUPPORTED),
+    (dict(cache=cache(head_dim=96)), EUNSUPPORTED)])
+def test_decode(change, code):
+    f = dict(cache=cache(), q=heads(), out=heads(), lens=P, window=0, scale=0.1, slots=bs.CacheSlots(P, P, 112), slots_out=bs.CacheSlots(P, P, 112), workspace=P, n_bytes=1 << 40)
+    f.update(change)
+    rc = binding.load_library().bs_attn_decode(ref(f["cache"]), ref(f["q"]), ref(f["out"]), f["lens"], f["window"], f["scale"], ref(f["slots"]), ref(f["slots_out"]),
+                                               f["workspace"], f["n_bytes"], None)
+    assert rc == code
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(lens=None), EINVAL), (dict(lens_out=None), EINVAL), (dict(keep=0), EINVAL), (dict(keep=-5), EINVAL), (dict(keep_first=-1), EINVAL), (dict(keep_last=-1), EINVAL),
+    (dict(keep_first=6, keep_last=5), EINVAL), (dict(keep_first=2 ** 31 - 1, keep_last=2 ** 31 - 1), EINVAL), (dict(slots=None), EINVAL), (dict(slots_out=None), EINVAL),
+    (dict(slots=bs.CacheSlots(P, None, 112)), EINVAL), (dict(slots_out=bs.CacheSlots(None, P, 112)), EINVAL), (dict(slots=bs.CacheSlots(P, P, 111)), EINVAL),
+    (dict(slots=bs.CacheSlots(P, P, 113)), EINVAL), (dict(workspace=None), EINVAL), (dict(workspace=P + 4), EINVAL), (dict(n_bytes=100), EINVAL)])
+def test_evict(change, code):
+    f = dict(lens=P, lens_out=P, keep=10, keep_first=0, keep_last=0, slots=bs.CacheSlots(P, P, 112), slots_out=bs.CacheSlots(P, P, 112), workspace=P, n_bytes=1 << 40)
+    f.update(change)
+    rc = binding.load_library().bs_cache_evict(ref(cache()), f["lens"], f["lens_out"], f["keep"], f["keep_first"], f["keep_last"], ref(f["slots"]), ref(f["slots_out"]),
+                                               f["workspace"], f["n_bytes"], None)
+    assert rc == code
+
+
+@pytest.mark.parametrize("change", [
+    dict(k=None), dict(v=None), dict(k=heads(8)), dict(v=heads(3)), dict(n=-1), dict(token_slot=None), dict(q=heads()), dict(q_out=heads()), dict(q=heads(), q_out=heads(4)),
+    dict(q=heads(), q_out=heads(), rope=None), dict(positions=None), dict(axis_stride=-1), dict(slots=bs.CacheSlots(P, P, 111)), dict(k=heads(4, P + 1)),
+    dict(rope=bs.bs_rope_init(130))])
+def test_append(change):
+    f = dict(k=heads(4), v=heads(4), n=3, token_slot=P, rope=bs.bs_rope_init(64), positions=P, axis_stride=3, q=None, q_out=None, slots=None)
+    f.update(change)
+    rc = binding.load_library().bs_cache_append(ref(cache()), ref(f["k"]), ref(f["v"]), f["n"], None, f["token_slot"], ref(f["rope"]), f["positions"], f["axis_stride"],
+                                                ref(f["q"]), ref(f["q_out"]), ref(f["slots"]), None, None)
+    assert rc == EINVAL
+
+
+def broken(**kw):
+    rope = bs.bs_rope_init(64)
+    for name, value in kw.items():
+        if name in ("freq", "axis"):
+            getattr(rope, name)[3] = value
+        else:
+            setattr(rope, name, value)
+    return rope
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(rope=None), EINVAL), (dict(x=None), EINVAL), (dict(n_tensors=0), EINVAL), (dict(n_tensors=3), EINVAL), (dict(dtype=2), EUNSUPPORTED), (dict(n=-1), EINVAL),
+    (dict(d=62), EINVAL), (dict(d=129), EINVAL), (dict(d=258), EINVAL), (dict(positions=None), EINVAL), (dict(axis_stride=-1), EINVAL), (dict(flags=2), EINVAL),
+    (dict(y=heads(7)), EINVAL), (dict(x=heads(data=P + 1)), EINVAL), (dict(x=heads(token=-1)), EINVAL), (dict(rope=broken(rotary_dim=63)), EINVAL),
+    (dict(rope=broken(rotary_dim=0)), EINVAL), (dict(rope=broken(layout=2)), EINVAL), (dict(rope=broken(n_axes=0)), EINVAL), (dict(rope=broken(n_axes=5)), EINVAL),
+    (dict(rope=broken(axis=1)), EINVAL), (dict(rope=broken(freq=math.nan)), EINVAL), (dict(rope=broken(freq=1e4)), EINVAL), (dict(rope=broken(magnitude=math.inf)), EINVAL)])
+def test_rope(change, code):
+    f = dict(rope=bs.bs_rope_init(64), x=heads(), y=heads(), n_tensors=1, dtype=bs.BS_BF16, n=3, d=128, positions=P, axis_stride=3, flags=0)
+    f.update(change)
+    rc = binding.load_library().bs_rope_apply(ref(f["rope"]), ref(f["x"]), ref(f["y"]), f["n_tensors"], f["dtype"], f["n"], f["d"], f["positions"], f["axis_stride"],
+                                              f["flags"], None)
+    assert rc == code
+
+
+@pytest.mark.parametrize("bad", [
+    dict(rotary_dim=0), dict(rotary_dim=63), dict(rotary_dim=258), dict(layout=2), dict(base=0.5), dict(base=math.nan), dict(scaling=4), dict(scaling=-1),
+    dict(scaling=bs.BS_ROPE_LINEAR, factor=0.5), dict(scaling=bs.BS_ROPE_BASE, rotary_dim=2, factor=2.0), dict(scaling=bs.BS_ROPE_PARTS, factor=2.0, original_len=0),
+    dict(scaling=bs.BS_ROPE_PARTS, factor=2.0, original_len=10, fast=1.0, slow=1.0), dict(magnitude=0.0), dict(magnitude=math.nan), dict(sections=[31]),
+    dict(sections=[33, -1]), dict(sections=[8, 8, 8, 4, 4]), dict(sections=[])])
+def test_rope_init(bad):
+    f = dict(rotary_dim=64)
+    f.update(bad)
+    with pytest.raises(bs.BlindsightError) as e:
+        bs.bs_rope_init(**f)
+    assert e.value.code == EINVAL
+
+
+def test_frequencies():
+    """fp64 powers and quotients: a few steps of 2^-53."""
+    i = np.arange(64)
+    f = 1e4 ** (-i / 64.0)
+    got = lambda **kw: np.array(bs.bs_rope_init(128, **kw).freq[:64])
+    assert np.allclose(got(), f, rtol=1e-14, atol=0)
+    assert np.allclose(got(scaling=bs.BS_ROPE_LINEAR, factor=4.0), f / 4, rtol=1e-14, atol=0)
+    b = got(scaling=bs.BS_ROPE_BASE, factor=4.0)
+    assert np.allclose(b, (1e4 * 4 ** (128 / 126)) ** (-i / 64.0), rtol=1e-13, atol=0) and abs(b[63] * 4 / f[63] - 1) < 1e-12   # the slowest pair: 1 / factor
+    g = np.clip((4096 * f / (2 * math.pi) - 1) / 31, 0, 1)
+    assert np.allclose(got(scaling=bs.BS_ROPE_PARTS, factor=4.0, original_len=4096), f * (g + (1 - g) / 4), rtol=1e-13, atol=0)
+    assert list(bs.bs_rope_init(64, sections=[0, 20, 12]).axis[:32]) == [1] * 20 + [2] * 12
+
+
+def test_views_that_the_binding_refuses():
+    torch = pytest.importorskip("torch")
+    with pytest.raises(ValueError):
+        bs.Heads.of(torch.zeros(2, 3, 8).transpose(1, 2))
+    k = torch.zeros(4, 2, 16, 64)
+    with pytest.raises(ValueError):
+        bs.KVCache.of(k, k[:3], torch.zeros((1, 2), dtype=torch.int32), bs.BS_F32)
+    with pytest.raises(ValueError):
+        bs.KVCache.of(k, k, torch.zeros((1, 2), dtype=torch.int64), bs.BS_F32)
+    with pytest.raises(ValueError):
+        bs.CacheSlots.of()
+    with pytest.raises(ValueError):
+        bs.CacheSlots.of(torch.zeros(1, 2, 5), torch.zeros((1, 2, 6), dtype=torch.int32))

@@ -1,0 +1,136 @@
+"""Rotary positions against a plain form in 64 bits.
+
+Tolerance per element, pair (a, b): the sine and cosine are off by at most 2 steps of 2^-24 (the reduced angle's rounding, the series, its
+last sum), the magnitude, each product and the sum by one more: 6 2^-24 (|a| + |b|) magnitude; the angle itself, a product of 64-bit numbers of
+at most |angle|, by 3 |angle| 2^-53; the result is rounded once, half a step of its type."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2507_09071_amd as bs
+from cache_util import DEV, HALF_STEP, TYPES, dtype_of, stream
+
+pytestmark = pytest.mark.gpu
+
+
+def plain(rope, x, positions, inverse):
+    """x [heads][tokens][d], positions [axes][tokens].  The rotated rows and their tolerance without the last rounding."""
+    x = x.astype(np.float64)
+    r = rope.rotary_dim
+    y, tol = x.copy(), np.zeros(x.shape)
+    for i in range(r // 2):
+        lo, hi = (i, i + r // 2) if rope.layout == bs.BS_ROPE_HALF else (2 * i, 2 * i + 1)
+        angle = positions[rope.axis[i]].astype(np.float64) * rope.freq[i]
+        m = float(np.float32(rope.magnitude))
+        c, s = np.cos(angle) * m, np.sin(angle) * m * (-1 if inverse else 1)
+        a, b = x[..., lo], x[..., hi]
+        y[..., lo], y[..., hi] = a * c - b * s, b * c + a * s
+        tol[..., lo] = tol[..., hi] = (np.abs(a) + np.abs(b)) * m * (6 * 2.0 ** -24 + 3 * np.abs(angle) * 2.0 ** -53)
+    return y, tol
+
+
+def check(got, rope, x, positions, inverse, dtype):
+    want, tol = plain(rope, x.double().numpy(), positions, inverse)
+    got = got.double().cpu().numpy()
+    r = rope.rotary_dim
+    assert (np.abs(got - want) <= tol * 1.01 + HALF_STEP[dtype] * (np.abs(want) + tol)).all(), float(np.abs(got - want).max())
+    assert (got[..., r:] == x.double().numpy()[..., r:]).all()
+
+
+def draw(h, t, d, dtype, seed=0):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return torch.randn((h, t, d), generator=g).to(TYPES[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", [bs.BS_ROPE_HALF, bs.BS_ROPE_INTERLEAVED])
+@pytest.mark.parametrize("d,r", [(128, 128), (64, 64), (128, 64), (64, 20), (128, 36), (256, 256), (6, 2), (80, 80), (72, 16), (2, 2), (250, 30)])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_layouts_and_sizes(dtype, layout, d, r, inverse):
+    rope = bs.bs_rope_init(r, layout, 1e4, magnitude=1.25)
+    q, k = draw(7, 13, d, dtype), draw(2, 13, d, dtype, 1)
+    pos = np.arange(13, dtype=np.int32)[None] * 97 + 3
+    ys = [torch.full_like(x, float("nan"), device=DEV) for x in (q, k)]
+    bs.bs_rope_apply(rope, [q.to(DEV), k.to(DEV)], ys, dtype_of(dtype), 13, d, torch.from_numpy(pos).to(DEV), inverse=inverse, stream=stream())
+    for x, y in zip((q, k), ys):
+        check(y, rope, x, pos, inverse, dtype)
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 63, 64, 65, 1000, 20011])
+def test_token_counts(tokens):
+    rope = bs.bs_rope_init(128, sections=[16, 24, 24], base=1e6)
+    x = draw(3, tokens, 128, "bf16")
+    pos = np.stack([np.arange(tokens), np.arange(tokens) // 60, np.arange(tokens) % 60]).astype(np.int32)
+    y = torch.empty_like(x, device=DEV)
+    bs.bs_rope_apply(rope, [x.to(DEV)], [y], bs.BS_BF16, tokens, 128, torch.from_numpy(pos).to(DEV), stream=stream())
+    check(y, rope, x, pos, False, "bf16")
+
+
+@pytest.mark.parametrize("heads", [1, 3, 40, 129])
+def test_head_counts(heads):
+    rope = bs.bs_rope_init(64)
+    x = draw(heads, 300, 64, "f32")
+    pos = np.arange(300, dtype=np.int32)[None]
+    y = torch.empty_like(x, device=DEV)
+    bs.bs_rope_apply(rope, [x.to(DEV)], [y], bs.BS_F32, 300, 64, torch.from_numpy(pos).to(DEV), stream=stream())
+    check(y, rope, x, pos, False, "f32")
+
+
+def test_far_and_negative_positions():
+    rope = bs.bs_rope_init(64, base=1e6)
+    pos = np.array([[0, 1, -1, 2 ** 31 - 1, -2 ** 31, 10 ** 9 + 7, 999983, -424242]], dtype=np.int64).astype(np.int32)
+    x = draw(2, 8, 64, "f32")
+    y = torch.empty_like(x, device=DEV)
+    bs.bs_rope_apply(rope, [x.to(DEV)], [y], bs.BS_F32, 8, 64, torch.from_numpy(pos).to(DEV), stream=stream())
+    check(y, rope, x, pos, False, "f32")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shift,pad", [(0, 8), (1, 0), (1, 3), (2, 2), (4, 4), (8, 1)])
+def test_strides_alignment_and_rows_between(dtype, shift, pad):
+    """Token-major rows with gaps, from an odd element on; what lies between the rows stays."""
+    heads, tokens, d = 5, 21, 64
+    rope = bs.bs_rope_init(64, bs.BS_ROPE_INTERLEAVED)
+    buf = torch.randn(shift + tokens * (heads * d + pad)).to(TYPES[dtype])
+    view = lambda b: b[shift:].view(tokens, heads * d + pad)[:, :heads * d].unflatten(1, (heads, d)).transpose(0, 1)
+    x = view(buf).contiguous()
+    pos = np.arange(tokens, dtype=np.int32)[None] + 1000
+    src, dst = buf.to(DEV), torch.full_like(buf, 7.0, device=DEV)
+    bs.bs_rope_apply(rope, [view(src)], [view(dst)], dtype_of(dtype), tokens, d, torch.from_numpy(pos).to(DEV), stream=stream())
+    check(view(dst).contiguous(), rope, x, pos, False, dtype)
+    assert (dst[:shift] == 7).all() and (dst[shift:].view(tokens, -1)[:, heads * d:] == 7).all()
+    bs.bs_rope_apply(rope, [view(src)], [view(src)], dtype_of(dtype), tokens, d, torch.from_numpy(pos).to(DEV), stream=stream())   # in place
+    assert torch.equal(view(src), view(dst))
+
+
+def test_gradient():
+    """The inverse is the transposed rotation: against differences of the forward call's plain form, and there and back."""
+    rope = bs.bs_rope_init(48, bs.BS_ROPE_HALF, 1e4, bs.BS_ROPE_PARTS, 4.0, 2048, 32.0, 1.0)
+    x, gy = draw(2, 9, 64, "f32"), draw(2, 9, 64, "f32", 1)
+    pos = (np.arange(9, dtype=np.int32) * 1111)[None]
+    p = torch.from_numpy(pos).to(DEV)
+    gx = torch.empty_like(gy, device=DEV)
+    bs.bs_rope_apply(rope, [gy.to(DEV)], [gx], bs.BS_F32, 9, 64, p, inverse=True, stream=stream())
+    rng = np.random.default_rng(0)
+    dx = rng.standard_normal(x.shape)
+    f = lambda z: float((plain(rope, z, pos, False)[0] * gy.double().numpy()).sum())
+    x64 = x.double().numpy()
+    slope = (f(x64 + 1e-3 * dx) - f(x64 - 1e-3 * dx)) / 2e-3   # f is linear: exact up to rounding
+    assert abs(slope - float((gx.double().cpu().numpy() * dx).sum())) <= 1e-4 * float(np.abs(dx * gx.double().cpu().numpy()).sum())
+    y, back = torch.empty_like(x, device=DEV), torch.empty_like(x, device=DEV)
+    bs.bs_rope_apply(rope, [x.to(DEV)], [y], bs.BS_F32, 9, 64, p, stream=stream())
+    bs.bs_rope_apply(rope, [y], [back], bs.BS_F32, 9, 64, p, inverse=True, stream=stream())
+    assert (back.cpu() - x).abs().max() <= 30 * 2.0 ** -24 * 2 * math.sqrt(2) * x.abs().max()
+
+
+def test_scaled_frequencies_reach_the_kernel():
+    for scaling in (bs.BS_ROPE_LINEAR, bs.BS_ROPE_BASE, bs.BS_ROPE_PARTS):
+        rope = bs.bs_rope_init(128, bs.BS_ROPE_HALF, 1e4, scaling, 8.0, 4096, magnitude=1.2)
+        x = draw(2, 50, 128, "f32")
+        pos = (np.arange(50, dtype=np.int32) * 991)[None]
+        y = torch.empty_like(x, device=DEV)
+        bs.bs_rope_apply(rope, [x.to(DEV)], [y], bs.BS_F32, 50, 128, torch.from_numpy(pos).to(DEV), stream=stream())
+        check(y, rope, x, pos, False, "f32")
