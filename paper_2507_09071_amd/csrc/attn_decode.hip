@@ -1,6 +1,24 @@
 // Attention of one new token per sequence over a paged cache.
+//
+// What has to be done is reading K and V of every visible slot once, so the bound is HBM: 4 d FLOP for every query head of a group
+// and slot are at most a few dozen per byte, which the matrix pipe does on the side.  How:
+//  * the query heads of a KV head are the free dimension of a 16x16 MFMA (one block of 16 rows, or two; groups of 32 beyond that), so K and
+//    V are read once for all of them;
+//  * the work of all sequences and KV heads ("items") is one row of blocks of 32 slots (16 in fp32: the same bytes), cut into equal
+//    shares, one per workgroup, wherever that falls.  Lengths are known on the device only, so every workgroup finds its share by itself, from a
+//    sum over the lengths.  A batch of very different lengths is balanced to within four blocks, and one long sequence fills the chip;
+//  * the four waves of a workgroup take every fourth block and run on their own: no barrier in the loop.  K and V blocks go from
+//    the pages to LDS with 16-byte LDS-direct loads, two blocks deep: 32 KB in flight per wave.  Page numbers come through the scalar cache,
+//    a step before they are needed.  Chunks of 16 bytes are exchanged within a row (XOR with its number) so that column reads are free of conflicts;
+//  * an item that lies within a share is finished there, another's parts are joined by a second, small kernel in a fixed order;
+//  * with weights, the scores are left in the workspace (4 bytes per head and slot, where K has 256) and a third kernel turns them
+//    into probabilities once the sums are known: reading K again would cost half as much as the attention.
+#include "attn_common.h"
+
 #include <algorithm>
 #include <cmath>
+#include <mutex>
+#include <type_traits>
 
 #include "device_map.h"
 #include "paged_cache.h"
@@ -8,7 +26,9 @@
 namespace bs {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+
+struct Share { int32_t item, last; };   // of a workgroup: the item that begins in its share and goes on behind it (-1: none), and the last workgroup that has a part of it
 
 struct DecodeArgs {
     bs_cache cache;
@@ -16,96 +36,693 @@ struct DecodeArgs {
     void *out;
     int64_t q_head, q_seq, out_head, out_seq;
     const int32_t *lens;
-    int32_t G, window;
-    float scale;
+    int32_t G, groups, window;    // heads per KV head; groups of rows that they make
+    int32_t rows;                 // rows of a partial result: at most 16 or 32
+    int32_t n_shares;
+    float scale_log2e;
+    float *part_o;                // [2 n_shares][rows][d]: of share w, 2 w the item that began before it, 2 w + 1 the one that goes on behind it
+    float2 *part_ml;              // reference point and sum
+    Share *shares;
+    // with weights
+    float *scores;                // [block][rows][slots of a block], times scale log2(e)
+    float *log_sums;              // [seq][query head], to base 2
     const float *weights;
     float *weights_out;
     int64_t in_stride, out_stride;
 };
 
-__device__ inline int64_t row_offset(const bs_cache &c, int seq, int head, int slot)   // -1: no page
+template <typename T, int D>
+struct Traits {
+    static constexpr int kKeys = sizeof(T) == 2 ? 32 : 16;    // slots of a block
+    static constexpr int kRowBytes = D * (int)sizeof(T);
+    static constexpr int kBlock = kKeys * kRowBytes;          // one block of K or V
+    static constexpr int kLoads = kBlock / 1024;              // LDS-direct instructions per block
+    static constexpr int kLoads16 = 16 * kRowBytes / 1024;    // ... per 16 slots, which lie in one page
+    static constexpr int kWave = 4 * kBlock;                  // two stages of K and V
+    static constexpr int kRing = kWaves * kWave;
+    static constexpr int kPerCu = D == 64 ? 2 : 1;            // workgroups per CU
+    static constexpr int kRowsMax = 32;
+    static constexpr int kQuery = kRing + kWaves * kRowsMax * 8;   // the query rows
+    static constexpr int kLds = kQuery + kRowsMax * kRowBytes;
+    // exchange of the 16-byte chunks of row r: rows that share their banks get different chunks
+    __device__ static int swizzle(int r) { return kRowBytes == 128 ? (r >> 1) & 7 : r & 15; }
+};
+
+// Blocks of a sequence that are visible, from block `first` on.
+struct Visible { int n, begin, first, blocks; };
+template <int KEYS>
+__device__ inline Visible visible(const DecodeArgs &a, int seq)
 {
-    const int page = c.page_table[(int64_t)seq * c.max_pages + slot / c.page_size];
-    if (page < 0 || page >= c.n_pages) return -1;
-    return page * c.page_stride + head * c.head_stride + (slot % c.page_size) * c.slot_stride;
+    Visible v;
+    v.n = max(0, min(scalar_load<int>(a.lens + seq), a.cache.max_pages * a.cache.page_size));
+    v.begin = a.window > 0 ? max(0, v.n - a.window) : 0;
+    v.first = v.begin / KEYS;
+    v.blocks = (v.n + KEYS - 1) / KEYS - v.first;
+    return v;
 }
 
-// One workgroup per sequence and KV head: scores of 256 slots at a time, a running maximum and sum, channels over the threads.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void decode_rows(const DecodeArgs a)
+// The share of this workgroup in the row of all blocks: items of a sequence one behind the other, sequences one behind the other.
+struct Place { int seq, item, block; };   // sequence, item of it, block of that
+struct Range { int begin, end; Place at; int each; };   // `each`: blocks of a share
+
+// `items` per sequence.  All threads of the workgroup; blocks of a share: a multiple of four.
+template <int KEYS>
+__device__ inline Range own_range(const DecodeArgs &a, int items, int share, int n_shares)
 {
-    __shared__ float q[256], p[kThreads], wave_max[4], acc[kThreads];
-    const int seq = blockIdx.x, head = blockIdx.y, tid = threadIdx.x, d = a.cache.head_dim;
-    const int n = max(0, min(a.lens[seq], a.cache.max_pages * a.cache.page_size)), begin = a.window > 0 ? max(0, n - a.window) : 0;
-    const T *k = static_cast<const T *>(a.cache.k), *v = static_cast<const T *>(a.cache.v);
-    const int64_t row = (int64_t)seq * a.cache.n_kv_heads + head;
-    const auto score = [&](int j) {
-        const int64_t at = j < n ? row_offset(a.cache, seq, head, j) : -1;
-        if (at < 0) return -INFINITY;
-        float s = 0.f;
-        for (int c = 0; c < d; ++c) s = fmaf(q[c], (float)k[at + c], s);
-        return s * a.scale;
+    __shared__ int wave_sums[kWaves], found[3];
+    const int tid = threadIdx.x, S = a.cache.n_seqs;
+    Range r;
+    int total;
+    if (S == 1) {
+        const Visible v = visible<KEYS>(a, 0);
+        total = v.blocks * items;
+        r.each = max(kWaves, ((total + n_shares - 1) / n_shares + kWaves - 1) / kWaves * kWaves);
+        r.begin = (int)min((int64_t)total, (int64_t)share * r.each);
+        r.end = min(total, r.begin + r.each);
+        r.at.seq = 0;
+        r.at.item = v.blocks > 0 ? r.begin / v.blocks : 0;
+        r.at.block = r.begin - r.at.item * v.blocks;
+        return r;
+    }
+    // a thread adds up a few sequences one behind the other
+    const int each = (S + kThreads - 1) / kThreads, s0 = min(S, tid * each), s1 = min(S, s0 + each);
+    const auto blocks_of = [&](int s) {
+        const int n = max(0, min(a.lens[s], a.cache.max_pages * a.cache.page_size)), begin = a.window > 0 ? max(0, n - a.window) : 0;
+        return ((n + KEYS - 1) / KEYS - begin / KEYS) * items;
     };
-    const auto block_max = [&](float x) {
-        for (int off = 32; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor(x, off, 64));
-        __syncthreads();
-        if ((tid & 63) == 0) wave_max[tid >> 6] = x;
-        __syncthreads();
-        return fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
+    int mine = 0;
+    for (int s = s0; s < s1; ++s) mine += blocks_of(s);
+    int upto = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int x = __shfl_up(upto, off, 64);
+        if ((tid & 63) >= off) upto += x;
+    }
+    if ((tid & 63) == 63) wave_sums[tid >> 6] = upto;
+    __syncthreads();
+    total = 0;
+    int before = upto - mine;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        before += w < (tid >> 6) ? wave_sums[w] : 0;
+        total += wave_sums[w];
+    }
+    r.each = max(kWaves, ((total + n_shares - 1) / n_shares + kWaves - 1) / kWaves * kWaves);
+    r.begin = (int)min((int64_t)total, (int64_t)share * r.each);
+    r.end = min(total, r.begin + r.each);
+    if (r.begin >= before && r.begin < before + mine) {
+        int left = r.begin - before, s = s0, n = blocks_of(s0);
+        while (left >= n) { left -= n; n = blocks_of(++s); }
+        const int blocks = n / items;
+        found[0] = s;
+        found[1] = left / blocks;
+        found[2] = left - left / blocks * blocks;
+    }
+    __syncthreads();
+    r.at.seq = __builtin_amdgcn_readfirstlane(found[0]);
+    r.at.item = __builtin_amdgcn_readfirstlane(found[1]);
+    r.at.block = __builtin_amdgcn_readfirstlane(found[2]);
+    r.begin = __builtin_amdgcn_readfirstlane(r.begin);
+    r.end = __builtin_amdgcn_readfirstlane(r.end);
+    r.each = __builtin_amdgcn_readfirstlane(r.each);
+    return r;
+}
+
+// The largest value, the sum, of the four lanes that hold the slots of one query row.
+__device__ inline float max_across_groups(float x)
+{
+    x = max_across_halves(x);
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float sum_across_groups(float x)
+{
+    x = sum_across_halves(x);
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ inline void store_row4(__bf16 *to, float4 x)
+{
+    bf16x4 w;
+    w[0] = (__bf16)x.x; w[1] = (__bf16)x.y; w[2] = (__bf16)x.z; w[3] = (__bf16)x.w;
+    *reinterpret_cast<bf16x4 *>(to) = w;
+}
+__device__ inline void store_row4(float *to, float4 x) { *reinterpret_cast<float4 *>(to) = x; }
+
+template <typename T, int D, int NRB, bool WEIGHTS>
+__global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void decode_shares(const DecodeArgs a)
+{
+    using TR = Traits<T, D>;
+    constexpr bool BF16 = sizeof(T) == 2;
+    constexpr int KEYS = TR::kKeys, ROWB = TR::kRowBytes, BLK = TR::kBlock, NI = TR::kLoads, NI16 = TR::kLoads16, SUB = KEYS / 16;
+    constexpr int ROWS = NRB * 16, NB = D / 16, CH4 = D / 4;
+    extern __shared__ __align__(1024) unsigned char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int items = a.cache.n_kv_heads * a.groups, P = a.cache.page_size;
+
+    // rows of sequences without a slot are zero
+    for (int s = blockIdx.x; s < a.cache.n_seqs; s += gridDim.x)
+        if (visible<KEYS>(a, s).n == 0)
+            for (int i = tid; i < a.G * a.cache.n_kv_heads * CH4; i += kThreads)
+                store_row4(static_cast<T *>(a.out) + s * a.out_seq + (i / CH4) * a.out_head + i % CH4 * 4, make_float4(0.f, 0.f, 0.f, 0.f));
+
+    const Range range = own_range<KEYS>(a, items, blockIdx.x, gridDim.x);
+    if (tid == 0) a.shares[blockIdx.x] = Share{-1, 0};
+    if (range.begin >= range.end) return;
+
+    typedef __attribute__((address_space(3))) void *lds_ptr;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr)lds, ring = lds0 + wave * TR::kWave;
+    // LDS-direct loads: instruction j of 16 slots moves 1 KB, i.e. 1024 / ROWB whole rows; a lane picks the chunk of its row that belongs at
+    // its place
+    uint32_t voff[NI16];
+#pragma unroll
+    for (int j = 0; j < NI16; ++j) {
+        const int r = j * (1024 / ROWB) + lane / (ROWB / 16), p = lane % (ROWB / 16);
+        voff[j] = r * (uint32_t)(a.cache.slot_stride * sizeof(T)) + ((p ^ TR::swizzle(r)) << 4);
+    }
+    const auto load_lds = [](uint32_t off, const char *src, uint32_t dst) __attribute__((always_inline)) {
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(src), "s"(dst) : "memory", "m0");
     };
-    for (int g = 0; g < a.G; ++g) {
-        const int h = head * a.G + g;
-        __syncthreads();
-        if (tid < d) q[tid] = (float)static_cast<const T *>(a.q)[seq * a.q_seq + h * a.q_head + tid];
-        __syncthreads();
-        float m = -INFINITY, l = 0.f, o = 0.f;   // o: channel tid % d, every (256 / d)-th slot
-        for (int j0 = begin; j0 < n; j0 += kThreads) {
-            const float s = score(j0 + tid), m_new = fmaxf(m, block_max(s));
-            const float alpha = m_new == -INFINITY ? 1.f : __expf(m - m_new);
-            p[tid] = m_new == -INFINITY ? 0.f : __expf(s - m_new);
-            m = m_new;
-            __syncthreads();
-            o *= alpha;
-            l *= alpha;
-            for (int i = tid / d; i < kThreads; i += kThreads / d) {
-                const int64_t at = j0 + i < n ? row_offset(a.cache, seq, head, j0 + i) : -1;
-                if (at < 0) continue;
-                o = fmaf(p[i], (float)v[at + tid % d], o);
-                l += p[i];
+    const auto wait_loads = [](auto newer) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(newer)::value) : "memory");
+    };
+    const auto reads_done = []() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+    // Stores of scores count among the loads in flight.  Those of the second row block are not counted: there may be none.
+    constexpr int NS = WEIGHTS ? SUB : 0;
+
+    const uint32_t k_read = wave * TR::kWave + col * ROWB + ((grp ^ TR::swizzle(col)) << 4);
+    uint32_t v_read[BF16 ? 2 : 4];   // bf16: of the two halves of a block; fp32: of the four slots of a lane
+    if constexpr (BF16) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = 16 * h + 4 * grp + (col >> 2);
+            v_read[h] = wave * TR::kWave + BLK + r * ROWB + ((((col >> 1) & 1) ^ TR::swizzle(r)) << 4) + (col & 1) * 8;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 4 * grp + i;
+            v_read[i] = wave * TR::kWave + BLK + r * ROWB + ((col ^ TR::swizzle(r)) << 4);
+        }
+    }
+
+    Place at = range.at;
+    int pos = range.begin;
+    Visible vis = visible<KEYS>(a, at.seq);
+    while (pos < range.end) {
+        while (at.item == items || vis.blocks == 0) {   // the next sequence that has some
+            at.item = 0;
+            vis = visible<KEYS>(a, ++at.seq);
+        }
+        const int blocks = min(vis.blocks - at.block, range.end - pos);
+        const int kvh = at.item / a.groups, row0 = kvh * a.G + (at.item - kvh * a.groups) * 32;
+        const int n_rows = min(ROWS, (kvh + 1) * a.G - row0);
+        const int n_steps = blocks > wave ? (blocks - wave + kWaves - 1) / kWaves : 0;
+        const int b0 = vis.first + at.block + wave;   // step i: block b0 + 4 i of the sequence
+
+        // Page numbers of 16 slots each; which slots of a block have a page.
+        const int32_t *table = a.cache.page_table + (int64_t)at.seq * a.cache.max_pages;
+        struct Pages { int32_t page[SUB]; uint32_t in_page[SUB]; };
+        const auto pages_of = [&](int i) __attribute__((always_inline)) {
+            Pages p;
+#pragma unroll
+            for (int h = 0; h < SUB; ++h) {
+                // (behind the last slots: those again)
+                const uint32_t slot = min((b0 + kWaves * min(i, n_steps - 1)) * KEYS + 16 * h, a.cache.max_pages * P - 16);
+                const uint32_t page = slot / (uint32_t)P;
+                p.page[h] = scalar_load<int>(table + page);
+                p.in_page[h] = slot - page * P;
+            }
+            return p;
+        };
+        struct Sources { const char *k[SUB], *v[SUB]; uint32_t there; };
+        const auto sources_of = [&](const Pages &p) __attribute__((always_inline)) {
+            Sources s;
+            s.there = 0;
+#pragma unroll
+            for (int h = 0; h < SUB; ++h) {
+                const bool ok = (uint32_t)p.page[h] < (uint32_t)a.cache.n_pages;
+                const int64_t off = ((ok ? p.page[h] : 0) * a.cache.page_stride + kvh * a.cache.head_stride + p.in_page[h] * a.cache.slot_stride) * (int64_t)sizeof(T);
+                s.k[h] = static_cast<const char *>(a.cache.k) + off;
+                s.v[h] = static_cast<const char *>(a.cache.v) + off;
+                s.there |= ok ? 0xffffu << (16 * h) : 0u;
+            }
+            return s;
+        };
+        const auto issue = [&](const char *const(&src)[SUB], uint32_t dst) __attribute__((always_inline)) {
+#pragma unroll
+            for (int h = 0; h < SUB; ++h)
+#pragma unroll
+                for (int j = 0; j < NI16; ++j) load_lds(voff[j], src[h], dst + (h * NI16 + j) * 1024);
+        };
+
+        // The query rows (the waves share them) in the layout of a K block, then the first two blocks of keys and values.  A slot without
+        // a row holds a copy of the last one, whose results are not stored.
+        {
+            const char *qh = reinterpret_cast<const char *>(static_cast<const T *>(a.q) + at.seq * a.q_seq + row0 * a.q_head);
+            constexpr int kAll = ROWS * ROWB / 1024;
+#pragma unroll
+            for (int i0 = 0; i0 < kAll; i0 += kWaves) {
+                const int i = i0 + wave;
+                if (kAll % kWaves == 0 || i < kAll) {
+                    const int r = i * (1024 / ROWB) + lane / (ROWB / 16), p = lane % (ROWB / 16);
+                    load_lds(min(r, n_rows - 1) * (uint32_t)(a.q_head * sizeof(T)) + ((p ^ TR::swizzle(r)) << 4), qh, lds0 + TR::kQuery + i * 1024);
+                }
+            }
+        }
+        Sources s0{}, s1{};
+        Pages next{};
+        if (n_steps > 0) {
+            const Pages p0 = pages_of(0), p1 = pages_of(1);
+            next = pages_of(2);
+            s0 = sources_of(p0);
+            issue(s0.k, ring);
+            issue(s0.v, ring + BLK);
+            s1 = sources_of(p1);
+            if (n_steps > 1) {
+                issue(s1.k, ring + 2 * BLK);
+                issue(s1.v, ring + 3 * BLK);
+                wait_loads(std::integral_constant<int, 4 * NI>{});
+            } else {
+                wait_loads(std::integral_constant<int, 2 * NI>{});
+            }
+        } else {
+            wait_loads(std::integral_constant<int, 0>{});
+        }
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        uint4 q[NRB][D * sizeof(T) / 64];
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+            for (int t = 0; t < (int)(D * sizeof(T) / 64); ++t)
+                q[rb][t] = *reinterpret_cast<const uint4 *>(lds + TR::kQuery + rb * 16 * ROWB + ((col * ROWB + ((grp ^ TR::swizzle(col)) << 4)) ^ (t << 6)));
+
+        floatx4 o[NRB][NB];
+        float m_run[NRB], l_run[NRB];
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+            m_run[rb] = -INFINITY;
+            l_run[rb] = 0.f;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[rb][nb][i] = 0.f;
+        }
+
+        uint32_t there0 = s0.there, there1 = s1.there;   // of this block, of the next one
+        for (int i = 0; i < n_steps; ++i) {
+            const int stage = (i & 1) * 2 * BLK;
+            const bool more = i + 1 < n_steps, more2 = i + 2 < n_steps;
+            const int n0 = (b0 + kWaves * i) * KEYS;
+            Sources s2{};
+            if (more2) s2 = sources_of(next);
+            next = pages_of(i + 3);
+
+            // ---- S^T = K Q^T: lane: slots 16 h + 4 grp + e of query row `col` of each row block
+            if (!more) wait_loads(std::integral_constant<int, NI>{});
+            else if (!WEIGHTS || i == 0) wait_loads(std::integral_constant<int, 3 * NI>{});
+            else wait_loads(std::integral_constant<int, 3 * NI + NS>{});
+            floatx4 s[NRB][SUB];
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+                for (int h = 0; h < SUB; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[rb][h][e] = 0.f;
+#pragma unroll
+            for (int t = 0; t < (int)(D * sizeof(T) / 64); ++t)
+#pragma unroll
+                for (int h = 0; h < SUB; ++h) {
+                    const uint4 f = *reinterpret_cast<const uint4 *>(lds + ((k_read + stage) ^ (t << 6)) + h * 16 * ROWB);
+#pragma unroll
+                    for (int rb = 0; rb < NRB; ++rb) {
+                        if constexpr (BF16) {
+                            s[rb][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, q[rb][t]), s[rb][h], 0, 0, 0);
+                        } else {
+                            const floatx4 x = __builtin_bit_cast(floatx4, f), y = __builtin_bit_cast(floatx4, q[rb][t]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[rb][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], s[rb][h], 0, 0, 0);
+                        }
+                    }
+                }
+            reads_done();
+            if (more2) issue(s2.k, ring + stage);
+
+            // ---- which of the lane's slots are seen (4 bits per 16 slots), and the running maximum and sum
+            uint32_t seen = there0;
+            if (n0 < vis.begin) seen &= ~0u << min(31, vis.begin - n0);   // (a block has a visible slot: vis.begin - n0 < KEYS)
+            if (n0 + KEYS > vis.n) seen &= ~(~0u << (vis.n - n0));
+            seen >>= 4 * grp;
+            float p[NRB][SUB][4];
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb) {
+                const float c = a.scale_log2e;
+                float mx = -INFINITY;
+#pragma unroll
+                for (int h = 0; h < SUB; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[rb][h][e] = (seen & (1u << (16 * h + e))) ? s[rb][h][e] : -INFINITY;
+                        mx = fmaxf(mx, s[rb][h][e]);
+                    }
+                if constexpr (WEIGHTS) {
+                    if (rb * 16 + col < n_rows) {
+                        float *to = a.scores + ((int64_t)(pos + wave + kWaves * i) * a.rows + rb * 16 + col) * KEYS + 4 * grp;
+#pragma unroll
+                        for (int h = 0; h < SUB; ++h)
+                            *reinterpret_cast<float4 *>(to + 16 * h) = make_float4(s[rb][h][0] * c, s[rb][h][1] * c, s[rb][h][2] * c, s[rb][h][3] * c);
+                    }
+                }
+                mx = max_across_groups(mx);
+                // the reference point moves only when the block's maximum exceeds it by 2^8 (any reference gives the same quotient),
+                // so the accumulators are rescaled a few times per row and not once per block
+                const bool grow = fmaf(mx, c, -(m_run[rb] * c)) > 8.f;
+                const float m_new = grow ? mx : m_run[rb];
+                const float off = m_new == -INFINITY ? 0.f : -(m_new * c);   // no slot so far: p = 0
+                const float alpha = grow ? __builtin_amdgcn_exp2f(fmaf(m_run[rb], c, off)) : 1.f;
+                float sum = 0.f;
+#pragma unroll
+                for (int h = 0; h < SUB; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p[rb][h][e] = __builtin_amdgcn_exp2f(fmaf(s[rb][h][e], c, off));
+                        sum += p[rb][h][e];
+                    }
+                l_run[rb] = fmaf(l_run[rb], alpha, sum);
+                m_run[rb] = m_new;
+                if (__any(alpha != 1.f)) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[rb][nb][e] *= alpha;
+                }
+            }
+
+            // ---- O^T += V^T P^T.  Values of slots that are not seen are replaced by zero: times a probability of zero, an infinity or a NaN would
+            // be a NaN.
+            if (more2) wait_loads(std::integral_constant<int, 3 * NI + NS>{});
+            else if (more) wait_loads(std::integral_constant<int, 2 * NI>{});
+            else wait_loads(std::integral_constant<int, 0>{});
+            if constexpr (BF16) {
+                typedef __attribute__((address_space(3))) bf16x4 *lds_bf16x4;
+                bf16x8 pb[NRB];
+#pragma unroll
+                for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) pb[rb][e] = (__bf16)p[rb][e >> 2][e & 3];
+                uint32_t keep[2][2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int w = 0; w < 2; ++w)
+                        keep[h][w] = ((seen >> (16 * h + 2 * w)) & 1 ? 0xffffu : 0u) | ((seen >> (16 * h + 2 * w + 1)) & 1 ? 0xffff0000u : 0u);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    uint4 f;
+                    const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(lds + ((v_read[0] + stage) ^ (nb << 5)))));
+                    const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(lds + ((v_read[1] + stage) ^ (nb << 5)))));
+                    f.x = x.x & keep[0][0]; f.y = x.y & keep[0][1];
+                    f.z = y.x & keep[1][0]; f.w = y.y & keep[1][1];
+#pragma unroll
+                    for (int rb = 0; rb < NRB; ++rb) o[rb][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), pb[rb], o[rb][nb], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)   // slot 4 grp + e
+#pragma unroll
+                    for (int n = 0; n < D / 64; ++n) {
+                        floatx4 x = *reinterpret_cast<const floatx4 *>(lds + v_read[e] + stage + n * 256);
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            x[w] = (seen & (1u << e)) ? x[w] : 0.f;
+#pragma unroll
+                            for (int rb = 0; rb < NRB; ++rb) o[rb][4 * n + w] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[w], p[rb][0][e], o[rb][4 * n + w], 0, 0, 0);
+                        }
+                    }
+            }
+            reads_done();
+            if (more2) issue(s2.v, ring + stage + BLK);
+            there0 = there1;
+            there1 = s2.there;
+        }
+
+        // ---- the four waves' results, each in its part of the ring; [row][chunks of 4 channels, exchanged]
+        float2 *ml = reinterpret_cast<float2 *>(lds + TR::kRing);   // [wave][row]
+        float4 *stage = reinterpret_cast<float4 *>(lds);
+        constexpr int kStageWave = TR::kWave / 16;
+        static_assert(ROWS * CH4 <= kStageWave, "a wave's rows in its part of the ring");
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+            const int row = rb * 16 + col;
+            const float l = sum_across_groups(l_run[rb]);
+            if (grp == 0) ml[wave * ROWS + row] = make_float2(m_run[rb], l);
+            if (row < n_rows) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    if constexpr (BF16) {   // channels 16 nb + 4 grp + i
+                        stage[wave * kStageWave + row * CH4 + ((nb * 4 + grp) ^ (row & (CH4 - 1)))] = make_float4(o[rb][nb][0], o[rb][nb][1], o[rb][nb][2], o[rb][nb][3]);
+                    } else {                // channel 64 n + 16 grp + 4 i + w of o[4 n + w][i]: here nb = 4 n + i
+                        const int n = nb / 4, i = nb % 4;
+                        stage[wave * kStageWave + row * CH4 + ((16 * n + 4 * grp + i) ^ (row & (CH4 - 1)))] =
+                            make_float4(o[rb][4 * n][i], o[rb][4 * n + 1][i], o[rb][4 * n + 2][i], o[rb][4 * n + 3][i]);
+                    }
+                }
             }
         }
         __syncthreads();
-        acc[tid] = o;
-        p[tid] = l;
-        __syncthreads();
-        float sum = 0.f;
-        l = 0.f;
-        for (int i = 0; i < kThreads / d; ++i) { sum += acc[i * d + tid % d]; l += p[i * d]; }
-        if (tid < d) static_cast<T *>(a.out)[seq * a.out_seq + h * a.out_head + tid] = (T)(n > begin && m > -INFINITY ? sum / l : (l == 0.f ? 0.f : l));
-        if (a.weights)
-            for (int j = tid; j < n; j += kThreads) {
-                const float s = score(j);
-                const float before = g == 0 ? a.weights[row * a.in_stride + j] : a.weights_out[row * a.out_stride + j];
-                a.weights_out[row * a.out_stride + j] = before + (s == -INFINITY ? 0.f : __expf(s - m) / l);
+        const bool begins = at.block == 0, ends = at.block + blocks == vis.blocks;
+        const int64_t slot = (int64_t)(2 * blockIdx.x + (begins ? 1 : 0)) * a.rows;
+        for (int idx = tid; idx < n_rows * CH4; idx += kThreads) {
+            const int row = idx / CH4, ch = idx % CH4;
+            float2 x[kWaves];
+            float4 y[kWaves];
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                x[w] = ml[w * ROWS + row];
+                y[w] = stage[w * kStageWave + row * CH4 + (ch ^ (row & (CH4 - 1)))];
             }
+            const float m = fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x));
+            float l = 0.f;
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = x[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[w].x - m) * a.scale_log2e);
+                l = fmaf(x[w].y, f, l);
+                sum.x = fmaf(y[w].x, f, sum.x); sum.y = fmaf(y[w].y, f, sum.y); sum.z = fmaf(y[w].z, f, sum.z); sum.w = fmaf(y[w].w, f, sum.w);
+            }
+            if (begins && ends) {
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                store_row4(static_cast<T *>(a.out) + at.seq * a.out_seq + (row0 + row) * a.out_head + 4 * ch, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+                if (WEIGHTS && ch == 0) a.log_sums[(int64_t)at.seq * a.cache.n_kv_heads * a.G + row0 + row] = l == 0.f ? 0.f : fmaf(m, a.scale_log2e, __builtin_amdgcn_logf(l));
+            } else {
+                *reinterpret_cast<float4 *>(a.part_o + (slot + row) * D + 4 * ch) = sum;
+                if (ch == 0) a.part_ml[slot + row] = make_float2(m, l);
+            }
+        }
+        if (begins && !ends && tid == 0) a.shares[blockIdx.x] = Share{at.seq * items + at.item, (pos + vis.blocks - 1) / range.each};
+        pos += blocks;
+        at.block = 0;
+        ++at.item;
+        if (pos < range.end) __syncthreads();   // the ring is free again
     }
+}
+
+// Joins the parts of the item that begins in share blockIdx.x and goes on behind it, row blockIdx.y: threads are D / 4 channel quads
+// times the parts side by side, in a fixed order.
+template <typename T, int D, bool WEIGHTS>
+__global__ __launch_bounds__(256) void decode_join(const DecodeArgs a)
+{
+    constexpr int CH4 = D / 4, LANES = 256 / CH4;
+    __shared__ float4 acc[LANES][CH4];
+    __shared__ float2 ml[LANES];
+    const int tid = threadIdx.x, ch = tid % CH4, p0 = tid / CH4, row = blockIdx.y;
+    const Share share = a.shares[blockIdx.x];
+    if (share.item < 0) return;
+    const int items = a.cache.n_kv_heads * a.groups, seq = share.item / items, item = share.item - seq * items;
+    const int kvh = item / a.groups, row0 = kvh * a.G + (item - kvh * a.groups) * 32;
+    if (row >= min(a.rows, (kvh + 1) * a.G - row0)) return;
+    float m = -INFINITY, l = 0.f;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int w = (int)blockIdx.x + p0; w <= share.last; w += LANES) {
+        const int64_t at = (int64_t)(2 * w + (w == (int)blockIdx.x ? 1 : 0)) * a.rows + row;
+        const float2 x = a.part_ml[at];
+        const float4 y = *reinterpret_cast<const float4 *>(a.part_o + at * D + 4 * ch);
+        const float m_new = fmaxf(m, x.x);
+        const float f0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * a.scale_log2e), f1 = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x.x - m_new) * a.scale_log2e);
+        l = l * f0 + x.y * f1;
+        sum.x = sum.x * f0 + y.x * f1; sum.y = sum.y * f0 + y.y * f1; sum.z = sum.z * f0 + y.z * f1; sum.w = sum.w * f0 + y.w * f1;
+        m = m_new;
+    }
+    acc[p0][ch] = sum;
+    if (ch == 0) ml[p0] = make_float2(m, l);
+    __syncthreads();
+    if (p0 != 0) return;
+    float m_all = -INFINITY;
+    for (int i = 0; i < LANES; ++i) m_all = fmaxf(m_all, ml[i].x);
+    l = 0.f;
+    sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < LANES; ++i) {
+        const float f = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[i].x - m_all) * a.scale_log2e);
+        l = fmaf(ml[i].y, f, l);
+        const float4 y = acc[i][ch];
+        sum.x = fmaf(y.x, f, sum.x); sum.y = fmaf(y.y, f, sum.y); sum.z = fmaf(y.z, f, sum.z); sum.w = fmaf(y.w, f, sum.w);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    store_row4(static_cast<T *>(a.out) + seq * a.out_seq + (row0 + row) * a.out_head + 4 * ch, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+    if (WEIGHTS && ch == 0) a.log_sums[(int64_t)seq * a.cache.n_kv_heads * a.G + row0 + row] = l == 0.f ? 0.f : fmaf(m_all, a.scale_log2e, __builtin_amdgcn_logf(l));
+}
+
+// What every slot received: a thread has a slot and adds up its KV head's rows, in order.
+template <int KEYS>
+__global__ __launch_bounds__(kThreads) void decode_weights(const DecodeArgs a)
+{
+    constexpr int kSide = kThreads / KEYS;   // blocks side by side
+    const int n_kv = a.cache.n_kv_heads, side = threadIdx.x / KEYS, key = threadIdx.x % KEYS;
+    const Range range = own_range<KEYS>(a, n_kv, blockIdx.x, gridDim.x);
+    Place at = range.at;
+    int pos = range.begin;
+    if (pos >= range.end) return;
+    Visible vis = visible<KEYS>(a, at.seq);
+    // where the sequence's blocks begin among those of all items
+    int64_t before = (int64_t)(pos - at.item * vis.blocks - at.block) * a.groups;
+    while (pos < range.end) {
+        while (at.item == n_kv || vis.blocks == 0) {
+            before += (int64_t)vis.blocks * n_kv * a.groups;
+            at.item = 0;
+            vis = visible<KEYS>(a, ++at.seq);
+        }
+        const int blocks = min(vis.blocks - at.block, range.end - pos);
+        const int64_t row = (int64_t)at.seq * n_kv + at.item;
+        const float *logs = a.log_sums + row * a.G;
+        for (int b = side; b < blocks; b += kSide) {
+            const int j = (at.block + b) * KEYS + key;
+            if (j >= vis.n) continue;
+            float sum = 0.f;
+            for (int g = 0; g < a.groups; ++g) {
+                const float *x = a.scores + (before + ((int64_t)at.item * a.groups + g) * vis.blocks + at.block + b) * a.rows * KEYS + key;
+                const int n_rows = min(a.rows, a.G - 32 * g);
+                for (int r = 0; r < n_rows; ++r) sum += __builtin_amdgcn_exp2f(x[r * KEYS] - logs[32 * g + r]);
+            }
+            a.weights_out[row * a.out_stride + j] = a.weights[row * a.in_stride + j] + sum;
+        }
+        pos += blocks;
+        at.block = 0;
+        ++at.item;
+    }
+}
+
+// ------------------------------------------------------------------------------------ host
+
+constexpr int kMaxDevices = 64;
+std::mutex g_mutex;
+int g_n_cus[kMaxDevices];   // compute units of a device, once its kernels' limits are raised
+
+template <typename T, int D>
+hipError_t raise_limits()
+{
+    const void *const kernels[] = {reinterpret_cast<const void *>(decode_shares<T, D, 1, false>), reinterpret_cast<const void *>(decode_shares<T, D, 2, false>),
+                                   reinterpret_cast<const void *>(decode_shares<T, D, 1, true>), reinterpret_cast<const void *>(decode_shares<T, D, 2, true>)};
+    for (const void *k : kernels)
+        if (const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, Traits<T, D>::kLds); e != hipSuccess) return e;
+    return hipSuccess;
+}
+
+int device_setup(int *n_cus)
+{
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return fail_hip(e, "hipGetDevice");
+    if (dev < 0 || dev >= kMaxDevices) return fail_msg(BS_EUNSUPPORTED, "device ordinal above 63");
+    std::lock_guard<std::mutex> lock(g_mutex);
+    if (g_n_cus[dev] == 0) {
+        e = raise_limits<__bf16, 64>();
+        if (e == hipSuccess) e = raise_limits<__bf16, 128>();
+        if (e == hipSuccess) e = raise_limits<float, 64>();
+        if (e == hipSuccess) e = raise_limits<float, 128>();
+        if (e != hipSuccess) return fail_hip(e, "hipFuncSetAttribute");
+        int cus = 0;
+        e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+        if (e != hipSuccess || cus <= 0) return fail_hip(e, "hipDeviceGetAttribute(compute units)");
+        g_n_cus[dev] = cus;
+    }
+    *n_cus = g_n_cus[dev];
+    return BS_OK;
 }
 
 int check_decode(const bs_cache *cache, int32_t n_q_heads)
 {
     if (int rc = check_cache(cache)) return rc;
     if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads != 0) return BS_EINVAL;
-    if ((cache->head_dim != 64 && cache->head_dim != 128) || cache->n_kv_heads > 65535) return BS_EUNSUPPORTED;
+    if (cache->head_dim != 64 && cache->head_dim != 128) return BS_EUNSUPPORTED;
     return BS_OK;
+}
+
+// How a call is laid out over the chip and its workspace.
+struct Plan {
+    int32_t groups, row_blocks, rows, n_shares;
+    int64_t blocks;                                         // at most
+    int64_t part_o, part_ml, shares, scores, log_sums, bytes;   // offsets
+};
+
+// Nothing but sizes, so that a graph of a call stays right when lengths change.
+int make_plan(const bs_cache &c, int32_t n_q_heads, bool weights, int n_cus, Plan *p)
+{
+    const int32_t G = n_q_heads / c.n_kv_heads, keys = c.dtype == BS_BF16 ? 32 : 16;
+    p->groups = (G + 31) / 32;
+    p->row_blocks = G > 16 ? 2 : 1;
+    p->rows = std::min(G, 32);
+    const int64_t per_item = (cache_slots(c) + keys - 1) / keys + 1;   // (a window may begin and end inside a block)
+    if ((int64_t)c.n_seqs * c.n_kv_heads > INT32_MAX / p->groups || (int64_t)c.n_seqs * c.n_kv_heads * p->groups > INT32_MAX / 2 / per_item) return BS_EUNSUPPORTED;
+    p->blocks = (int64_t)c.n_seqs * c.n_kv_heads * p->groups * per_item;
+    p->n_shares = (int32_t)std::min<int64_t>((int64_t)n_cus * (c.head_dim == 64 ? 2 : 1), (p->blocks + kWaves - 1) / kWaves);
+    const auto whole = [](int64_t bytes) { return (bytes + 255) / 256 * 256; };
+    p->part_o = 0;
+    p->part_ml = whole((int64_t)2 * p->n_shares * p->rows * c.head_dim * 4);
+    p->shares = p->part_ml + whole((int64_t)2 * p->n_shares * p->rows * 8);
+    p->scores = p->shares + whole((int64_t)p->n_shares * sizeof(Share));
+    p->log_sums = p->scores + (weights ? whole(p->blocks * p->rows * keys * 4) : 0);
+    p->bytes = p->log_sums + (weights ? whole((int64_t)c.n_seqs * n_q_heads * 4) : 0);
+    return BS_OK;
+}
+
+template <typename T, int D, bool WEIGHTS>
+int launch(const DecodeArgs &a, const Plan &p, int n_cus, hipStream_t st)
+{
+    const dim3 grid((unsigned)p.n_shares), block(kThreads);
+    hipError_t e = p.row_blocks == 1 ? launch_kernel(decode_shares<T, D, 1, WEIGHTS>, grid, block, Traits<T, D>::kLds, st, a)
+                                     : launch_kernel(decode_shares<T, D, 2, WEIGHTS>, grid, block, Traits<T, D>::kLds, st, a);
+    if (e != hipSuccess) return fail_hip(e, "decode_shares launch");
+    if (p.n_shares > 1) e = launch_kernel(decode_join<T, D, WEIGHTS>, dim3((unsigned)p.n_shares, (unsigned)p.rows), dim3(256), 0, st, a);
+    if (e != hipSuccess) return fail_hip(e, "decode_join launch");
+    if constexpr (WEIGHTS) {
+        const int64_t wgs = std::min<int64_t>((int64_t)n_cus * 8, (p.blocks / p.groups + 3) / 4);
+        e = launch_kernel(decode_weights<Traits<T, D>::kKeys>, dim3((unsigned)wgs), block, 0, st, a);
+        if (e != hipSuccess) return fail_hip(e, "decode_weights launch");
+    }
+    return BS_OK;
+}
+
+template <typename T, int D>
+int launch(const DecodeArgs &a, const Plan &p, int n_cus, hipStream_t st)
+{
+    return a.weights ? launch<T, D, true>(a, p, n_cus, st) : launch<T, D, false>(a, p, n_cus, st);
 }
 
 }  // namespace
 }  // namespace bs
 
-extern "C" int64_t bs_attn_decode_workspace(const bs_cache *cache, int32_t n_q_heads, int32_t)
+extern "C" int64_t bs_attn_decode_workspace(const bs_cache *cache, int32_t n_q_heads, int32_t with_weights)
 {
-    if (int rc = bs::check_decode(cache, n_q_heads)) return rc;
-    return 0;
+    using namespace bs;
+    if (int rc = check_decode(cache, n_q_heads)) return rc;
+    int n_cus = 0;
+    Plan p;
+    if (int rc = device_setup(&n_cus)) return rc;
+    if (int rc = make_plan(*cache, n_q_heads, with_weights != 0, n_cus, &p)) return rc;
+    return p.bytes;
 }
 
 extern "C" int bs_attn_decode(const bs_cache *cache, const bs_heads *q, const bs_heads *out, const int32_t *lens, int32_t window, float scale,
@@ -114,28 +731,41 @@ extern "C" int bs_attn_decode(const bs_cache *cache, const bs_heads *q, const bs
     using namespace bs;
     if (check_heads(q) || check_heads(out) || q->n_heads != out->n_heads || !lens || window < 0 || !(scale > 0.f) || !std::isfinite(scale)) return BS_EINVAL;
     if (int rc = check_decode(cache, q->n_heads)) return rc;
-    if (!slots != !slots_out || !workspace || (uintptr_t)workspace % 16 != 0) return BS_EINVAL;
+    if (!slots != !slots_out || !workspace || (uintptr_t)workspace % 16 != 0 || workspace_bytes < 0) return BS_EINVAL;
     if (slots) {
         if (!slots->weights || !slots_out->weights || check_slots(*cache, slots) || check_slots(*cache, slots_out)) return BS_EINVAL;
         if (slots->weights == slots_out->weights && slots->row_stride != slots_out->row_stride) return BS_EINVAL;
         if (window > 0) return BS_EUNSUPPORTED;
     }
     if (!rows_aligned(*q, cache->dtype) || !rows_aligned(*out, cache->dtype)) return BS_EUNSUPPORTED;
-    if (workspace_bytes < bs_attn_decode_workspace(cache, q->n_heads, slots != nullptr)) return BS_EINVAL;
+    if (q->head_stride * element_bytes(cache->dtype) * 32 > INT32_MAX) return BS_EUNSUPPORTED;   // rows of a group are addressed in 32 bits
+    int n_cus = 0;
+    Plan p;
+    if (int rc = device_setup(&n_cus)) return rc;
+    if (int rc = make_plan(*cache, q->n_heads, slots != nullptr, n_cus, &p)) return rc;
+    if (workspace_bytes < p.bytes) return BS_EINVAL;
     DecodeArgs a{};
     a.cache = *cache;
     a.q = q->data; a.q_head = q->head_stride; a.q_seq = q->token_stride;
     a.out = out->data; a.out_head = out->head_stride; a.out_seq = out->token_stride;
     a.lens = lens;
     a.G = q->n_heads / cache->n_kv_heads;
+    a.groups = p.groups;
     a.window = window;
-    a.scale = scale;
+    a.rows = p.rows;
+    a.n_shares = p.n_shares;
+    a.scale_log2e = scale * 1.4426950408889634f;
+    char *ws = static_cast<char *>(workspace);
+    a.part_o = reinterpret_cast<float *>(ws + p.part_o);
+    a.part_ml = reinterpret_cast<float2 *>(ws + p.part_ml);
+    a.shares = reinterpret_cast<Share *>(ws + p.shares);
     if (slots) {
+        a.scores = reinterpret_cast<float *>(ws + p.scores);
+        a.log_sums = reinterpret_cast<float *>(ws + p.log_sums);
         a.weights = slots->weights; a.in_stride = slots->row_stride;
         a.weights_out = slots_out->weights; a.out_stride = slots_out->row_stride;
     }
-    const dim3 grid((unsigned)cache->n_seqs, (unsigned)cache->n_kv_heads);
-    const hipError_t e = cache->dtype == BS_BF16 ? launch_kernel(decode_rows<__bf16>, grid, dim3(kThreads), 0, (hipStream_t)stream, a)
-                                                 : launch_kernel(decode_rows<float>, grid, dim3(kThreads), 0, (hipStream_t)stream, a);
-    return e == hipSuccess ? BS_OK : fail_hip(e, "decode_rows launch");
+    hipStream_t st = (hipStream_t)stream;
+    if (cache->dtype == BS_BF16) return cache->head_dim == 64 ? launch<__bf16, 64>(a, p, n_cus, st) : launch<__bf16, 128>(a, p, n_cus, st);
+    return cache->head_dim == 64 ? launch<float, 64>(a, p, n_cus, st) : launch<float, 128>(a, p, n_cus, st);
 }
