@@ -1,11 +1,16 @@
 // Eviction from a paged cache by accumulated attention weight.
 //
 // Per sequence and KV head ("row") the `keep` slots with the largest weights stay.  Weights are ranked as unsigned integers of the same
-// order, protected slots above all; the rank of the last one kept is found digit by digit from counts (radix selection), ties go
-// to the lowest slots.  Kept slots behind `keep` move into the holes before it: the two sets do not overlap, so moves need
-// no order among each other, and nothing moves that can stay.  Weights and orders are read once per pass over them (8 bytes a slot),
-// moves cost 4 rows each.
+// order, protected slots above all; the rank of the last one kept is found from counts of its digits, 11, 11 and 10 bits from the top, and
+// ties go to the lowest slots.  The first digit is sign, exponent and two bits of the fraction, over which weights spread well, so that few
+// lanes of a wave count in the same place; mostly the second one leaves no more slots than are needed, and the third is not looked at.
+// Kept slots behind `keep` move into the holes before it: the two sets do not overlap, so moves need no order among each other, and nothing
+// moves that can stay.  Weights and orders are read once or twice (8 bytes a slot), moves cost 4 rows each.
+//
+// Two ways to select.  One workgroup per row with the row's ranks in LDS: one launch, all the chip where there are many rows.  Or a row cut into
+// chunks for many workgroups, with a launch per pass: few long rows.
 #include <algorithm>
+#include <mutex>
 
 #include "device_map.h"
 #include "paged_cache.h"
@@ -13,7 +18,8 @@
 namespace bs {
 namespace {
 
-constexpr int kSelectThreads = 1024, kMoveThreads = 256;
+constexpr int kMoveThreads = 256, kChunkThreads = 256;
+constexpr int kBins = 2048, kDigits = 3;   // of digits of at most 11 bits
 
 struct EvictArgs {
     bs_cache cache;
@@ -26,8 +32,16 @@ struct EvictArgs {
     int32_t *order_out;
     int64_t in_stride, out_stride;
     int32_t *counts;            // moves of each row
-    int32_t *to, *from;         // [row][max_moves]
+    int32_t *moves;             // [row][2 max_moves]: the slots moved into, then those they come from
     int32_t max_moves;
+    // rows in chunks
+    int32_t chunks;
+    int32_t *need;              // of each row, how many ties stay
+    int32_t *newest;            // [row][chunk] largest order
+    int32_t *hist;              // [row][digit][bin]
+    uint64_t *above, *ties;     // [row][words] slots that stay, and of those with the rank of the last one, a bit each
+    int4 *marked;               // [row][chunk] how many of them: above in front of `keep` and behind, ties in front and behind
+    int32_t words;
 };
 
 __device__ inline int used_slots(const EvictArgs &a, int seq)
@@ -44,101 +58,510 @@ __device__ inline uint32_t rank_of(float w, bool safe)
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// Sums x over the threads before this one; *total over all of them.  Two barriers.
-__device__ inline int before_in_block(bool x, int *wave_sums, int *total)
+struct Row {
+    const float *w;
+    const int32_t *order;
+    float *w_out;
+    int32_t *order_out;
+    int n;
+    __device__ Row(const EvictArgs &a, int row)
+        : w(a.weights + row * a.in_stride), order(a.order + row * a.in_stride), w_out(a.weights_out + row * a.out_stride),
+          order_out(a.order_out + row * a.out_stride), n(used_slots(a, row / a.cache.n_kv_heads)) {}
+    __device__ bool moves_out() const { return w_out != w || order_out != order; }
+    __device__ void leave(int j, float x, int32_t o) const   // a slot that stays where it is
+    {
+        if (w_out != w) w_out[j] = x;
+        if (order_out != order) order_out[j] = o;
+    }
+};
+
+// f(slots of eight of them) for the thread's slots from `begin` on, THREADS apart: loads of eight slots go out together, those behind the end
+// to the last slot.
+template <int THREADS, typename F>
+__device__ inline void for_eights(int begin, int end, F f)
+{
+    for (int j0 = begin; j0 < end; j0 += 8 * THREADS) {   // (uniform: `begin` is)
+        int j[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) j[e] = j0 + e * THREADS + (int)threadIdx.x;
+        f(j);
+    }
+}
+
+// Sum over the lanes up to this one.
+__device__ inline int wave_upto(int x)
+{
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(x, off, 64);
+        if ((int)(threadIdx.x & 63) >= off) x += y;
+    }
+    return x;
+}
+
+__device__ inline int wave_sum(int x)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
+    return x;
+}
+
+__device__ inline int wave_max(int x)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) x = max(x, __shfl_xor(x, off, 64));
+    return x;
+}
+
+template <int THREADS>
+struct Sums { int wave[THREADS / 64]; };
+
+// Exclusive sum over the threads; *total.  Two barriers.
+template <int THREADS>
+__device__ inline int sum_before(Sums<THREADS> &l, int x, int *total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint64_t b = __ballot(x);
-    if (lane == 0) wave_sums[wave] = __popcll(b);
+    const int upto = wave_upto(x);
+    if (lane == 63) l.wave[wave] = upto;
     __syncthreads();
     int before = 0, all = 0;
 #pragma unroll
-    for (int w = 0; w < kSelectThreads / 64; ++w) {
-        const int n = wave_sums[w];
+    for (int w = 0; w < THREADS / 64; ++w) {
+        const int n = l.wave[w];
         before += w < wave ? n : 0;
         all += n;
     }
     __syncthreads();
     *total = all;
-    return before + __popcll(b & ((1ull << lane) - 1));
+    return before + upto - x;
 }
 
-__global__ __launch_bounds__(kSelectThreads) void evict_select(const EvictArgs a)
+// How far the rank of the last slot kept is known: its bits from `shift` up; `need` of the in_bin slots that have these bits stay, and all
+// that have larger ones.
+struct Known {
+    uint32_t prefix;
+    int shift, need, in_bin;
+    __device__ Known(int keep, int n) : prefix(0), shift(32), need(keep), in_bin(n) {}
+    __device__ bool done() const { return shift == 0 || in_bin == need; }
+    __device__ int bits() const { return shift == 10 ? 10 : 11; }   // of the next digit
+    __device__ bool candidate(uint32_t r) const { return shift == 32 || (r >> shift) == prefix; }
+    __device__ bool larger(uint32_t r) const { return shift != 32 && (r >> shift) > prefix; }
+    __device__ int bin(uint32_t r) const { return (r >> (shift - bits())) & ((1 << bits()) - 1); }
+};
+
+// Of each digit, so that the next one need not wait until this one's have been read.
+template <int THREADS>
+struct DigitLds {
+    int wave[kDigits][THREADS / 64];
+    int digit[kDigits], need[kDigits], in_bin[kDigits];
+};
+
+// Counts a slot in `hist` (LDS).  A wave whose slots all count in one place adds them at once.
+__device__ inline void count_in(int *hist, bool counts, int bin)
 {
-    __shared__ int hist[256];
-    __shared__ int sums[kSelectThreads / 64];
-    __shared__ int shared_digit, shared_need, shared_newest;
-    const int row = blockIdx.x, tid = threadIdx.x;
-    const int n = used_slots(a, row / a.cache.n_kv_heads);
-    const float *w = a.weights + row * a.in_stride;
-    const int32_t *ord = a.order + row * a.in_stride;
-    float *w_out = a.weights_out + row * a.out_stride;
-    int32_t *ord_out = a.order_out + row * a.out_stride;
-    if (n <= a.keep) {
-        for (int j = tid; j < n; j += kSelectThreads) {
-            if (w_out != w) w_out[j] = w[j];
-            if (ord_out != ord) ord_out[j] = ord[j];
+    const uint64_t who = __ballot(counts);
+    if (who == 0) return;
+    const int first = __builtin_amdgcn_readlane(bin, __builtin_ctzll(who));
+    if (__ballot(counts && bin != first) == 0) {
+        if ((threadIdx.x & 63) == 0) atomicAdd(&hist[first], __popcll(who));
+    } else if (counts) {
+        atomicAdd(&hist[bin], 1);
+    }
+}
+
+// The next digit, from the counts of all its values.  Two barriers.
+template <int THREADS>
+__device__ inline void next_digit(DigitLds<THREADS> &l, const int *hist, Known &k)
+{
+    constexpr int EACH = kBins / THREADS;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i_digit = (32 - k.shift) / 11;
+    int x[EACH], mine = 0;   // from the largest digit down
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        x[i] = hist[kBins - 1 - (int)threadIdx.x * EACH - i];
+        mine += x[i];
+    }
+    const int upto = wave_upto(mine);
+    if (lane == 63) l.wave[i_digit][wave] = upto;
+    __syncthreads();
+    int left = k.need - upto + mine;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) left -= w < wave ? l.wave[i_digit][w] : 0;
+    if (left > 0 && left <= mine) {
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (!found && left <= x[i]) {
+                found = true;
+                l.digit[i_digit] = kBins - 1 - (int)threadIdx.x * EACH - i;
+                l.need[i_digit] = left;
+                l.in_bin[i_digit] = x[i];
+            }
+            if (!found) left -= x[i];
         }
+    }
+    __syncthreads();
+    const int bits = k.bits();
+    k.prefix = (k.shift == 32 ? 0 : k.prefix << bits) | (uint32_t)l.digit[i_digit];
+    k.shift -= bits;
+    k.need = l.need[i_digit];
+    k.in_bin = l.in_bin[i_digit];
+}
+
+__device__ inline bool is_safe(const EvictArgs &a, int32_t order, int32_t newest)
+{
+    return order < a.keep_first || (int64_t)order > (int64_t)newest - a.keep_last;
+}
+
+// ------------------------------------------------------------------------------------ one workgroup per row
+
+constexpr int kRanksMax = 32768;   // 128 KB of LDS
+
+// SHORT: a thread has at most eight slots and keeps them in registers.  Else ranks lie in LDS, and orders and weights are read again.
+template <int THREADS, bool SHORT>
+// (two rows of 1024 threads share a CU)
+__global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void evict_select(const EvictArgs a)
+{
+    constexpr int kFlags = (SHORT ? 8 * THREADS : kRanksMax) / 64;
+    __shared__ int hist[kDigits * kBins];
+    __shared__ DigitLds<THREADS> digits;
+    __shared__ Sums<THREADS> sums;
+    __shared__ int flags[kFlags];   // of each 64 slots, how many; then how many before
+    __shared__ int newest_lds;
+    extern __shared__ uint32_t ranks[];
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+    const Row r(a, row);
+    const int n = r.n;
+    if (n <= a.keep) {
+        for (int j = tid; j < n; j += THREADS) r.leave(j, r.w[j], r.order[j]);
         if (tid == 0) a.counts[row] = 0;
         return;
     }
-    if (tid == 0) shared_newest = INT32_MIN;
-    __syncthreads();
-    int newest = INT32_MIN;
-    for (int j = tid; j < n; j += kSelectThreads) newest = max(newest, ord[j]);
-    atomicMax(&shared_newest, newest);
-    __syncthreads();
-    newest = shared_newest;
-    const auto rank = [&](int j) {
-        const int32_t o = ord[j];
-        return rank_of(w[j], o < a.keep_first || (int64_t)o > (int64_t)newest - a.keep_last);
+    uint32_t rank[8];
+    int32_t o[8];
+    float x[8];
+    const auto load = [&](const int (&j)[8]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            o[e] = r.order[min(j[e], n - 1)];
+            x[e] = r.w[min(j[e], n - 1)];
+        }
     };
-    // the rank of the last slot kept: digits of 8 bits from the top
-    uint32_t prefix = 0;
-    int need = a.keep;   // slots still to be found among those whose higher digits are `prefix`
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
+    // f(slot, its rank), for all slots; slots behind the last one have no bit set in what f forms of them
+    const auto for_slots = [&](auto f) __attribute__((always_inline)) {
+        if constexpr (SHORT) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e * THREADS < n) f(e * THREADS + tid, rank[e]);
+        } else {
+            for (int j0 = 0; j0 < n; j0 += THREADS) f(j0 + tid, ranks[j0 + tid]);   // (there is room for whole rounds)
+        }
+    };
+    if (tid == 0) newest_lds = INT32_MIN;
+    int newest = INT32_MIN;
+    for_eights<THREADS>(0, n, [&](const int (&j)[8]) {
+        load(j);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            newest = max(newest, o[e]);
+            if constexpr (!SHORT) { if (j[e] < n) ranks[j[e]] = rank_of(x[e], false); }
+        }
+    });
+    for (int i = tid; i < kDigits * kBins; i += THREADS) hist[i] = 0;
+    __syncthreads();
+    newest = wave_max(newest);
+    if (lane == 0) atomicMax(&newest_lds, newest);
+    __syncthreads();
+    newest = newest_lds;
+    if constexpr (SHORT) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rank[e] = rank_of(x[e], is_safe(a, o[e], newest));
+    } else {
+        for_eights<THREADS>(0, n, [&](const int (&j)[8]) {   // (a thread's own slots)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = r.order[min(j[e], n - 1)];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (j[e] < n && is_safe(a, o[e], newest)) ranks[j[e]] = ~0u;
+        });
+    }
+    Known known(a.keep, n);
+    for (int digit = 0; digit < kDigits && !known.done(); ++digit) {
+        for_slots([&](int j, uint32_t &u) { count_in(hist + digit * kBins, j < n && known.candidate(u), known.bin(u)); });
         __syncthreads();
-        for (int j = tid; j < n; j += kSelectThreads) {
-            const uint32_t r = rank(j);
-            if (shift == 24 || (r >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(r >> shift) & 255], 1);
+        next_digit(digits, hist + digit * kBins, known);
+    }
+
+    // How many slots with a flag lie before each 64 of them: counts, then their sum in the order of slots.
+    int total;
+    const auto count_flags = [&](auto flag) __attribute__((always_inline)) {
+        for_slots([&](int j, uint32_t &u) {
+            const uint64_t b = __ballot(flag(j, u));
+            if (lane == 0 && j < n) flags[j / 64] = __popcll(b);
+        });
+        __syncthreads();
+        constexpr int EACH = (kFlags + THREADS - 1) / THREADS;
+        const int entries = (n + 63) / 64;
+        int mine = 0, c[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            c[i] = tid * EACH + i < entries ? flags[tid * EACH + i] : 0;
+            mine += c[i];
+        }
+        int before = sum_before(sums, mine, &total);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (tid * EACH + i < entries) flags[tid * EACH + i] = before;
+            before += c[i];
         }
         __syncthreads();
-        if (tid == 0) {
-            int d = 255, left = need;
-            while (hist[d] < left) left -= hist[d--];
-            shared_digit = d;
-            shared_need = left;
+    };
+    const auto flags_before = [&](int j, bool flag) {
+        const uint64_t b = __ballot(flag);
+        return flags[min(j, n - 1) / 64] + __popcll(b & ((1ull << lane) - 1));
+    };
+    // Of equal ranks the lowest slots stay.  From here on all that matters of a rank is whether its slot stays.
+    const bool ties = known.in_bin > known.need;
+    if (ties) count_flags([&](int j, uint32_t u) { return j < n && known.candidate(u); });
+    for_slots([&](int j, uint32_t &u) {
+        const bool tie = j < n && known.candidate(u);
+        bool stays = tie;
+        if (ties) {
+            const int before = flags_before(j, tie);
+            stays = tie && before < known.need;
         }
+        u = j < n && (stays || known.larger(u));
+    });
+    __syncthreads();
+    // Holes (evicted in front) and slots that move (kept behind) in one list: as many of the one as of the other.
+    const auto listed = [&](int j, uint32_t stays) { return j < n && (j < a.keep) == (stays == 0); };
+    count_flags(listed);
+    int32_t *moves = a.moves + (int64_t)row * 2 * a.max_moves;
+    for_slots([&](int j, uint32_t &u) {
+        const bool in_list = listed(j, u);
+        const int at = flags_before(j, in_list);
+        if (in_list) moves[at] = j;
+    });
+    if (tid == 0) a.counts[row] = total / 2;
+    if (r.moves_out())
+        for_eights<THREADS>(0, a.keep, [&](const int (&j)[8]) {
+            if constexpr (!SHORT) load(j);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t stays = SHORT ? rank[e] : ranks[min(j[e], n - 1)];
+                if (j[e] < a.keep && stays) r.leave(j[e], x[e], o[e]);
+            }
+        });
+}
+
+// ------------------------------------------------------------------------------------ rows in chunks
+
+// Slots [begin, end) of chunk blockIdx.y, whole 64s.
+struct Chunk {
+    int begin, end;
+    __device__ Chunk(const EvictArgs &a, int n)
+    {
+        const int words = (n + 63) / 64, each = (words + a.chunks - 1) / a.chunks;
+        begin = min(n, (int)blockIdx.y * each * 64);
+        end = min(n, begin + each * 64);
+    }
+};
+
+__global__ __launch_bounds__(kChunkThreads) void evict_newest(const EvictArgs a)
+{
+    __shared__ int waves[kChunkThreads / 64];
+    const int row = blockIdx.x, tid = threadIdx.x;
+    const Row r(a, row);
+    const Chunk c(a, r.n);
+    for (int i = (int)blockIdx.y * kChunkThreads + tid; i < kDigits * kBins; i += (int)gridDim.y * kChunkThreads) a.hist[(int64_t)row * kDigits * kBins + i] = 0;
+    if (r.n <= a.keep) {   // (the kernels behind have nothing to do then)
+        if (r.moves_out())
+            for (int j = c.begin + tid; j < c.end; j += kChunkThreads) r.leave(j, r.w[j], r.order[j]);
+        if (blockIdx.y == 0 && tid == 0) a.counts[row] = 0;
+        return;
+    }
+    int newest = INT32_MIN;
+    for_eights<kChunkThreads>(c.begin, c.end, [&](const int (&j)[8]) {
+        int32_t o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = r.order[min(j[e], c.end - 1)];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) newest = max(newest, o[e]);
+    });
+    newest = wave_max(newest);
+    if ((tid & 63) == 0) waves[tid >> 6] = newest;
+    __syncthreads();
+    if (tid == 0) a.newest[(int64_t)row * a.chunks + blockIdx.y] = max(max(waves[0], waves[1]), max(waves[2], waves[3]));
+}
+
+// The largest order of the row, from those of its chunks (fewer than there are threads in a wave: chunks <= 64).
+__device__ inline int32_t newest_of(const EvictArgs &a, int row)
+{
+    const int lane = threadIdx.x & 63;
+    return wave_max(lane < a.chunks ? a.newest[(int64_t)row * a.chunks + lane] : INT32_MIN);
+}
+
+// What is known of the last rank after `n_digits` digits have been counted.
+__device__ inline Known known_after(DigitLds<kChunkThreads> &l, const EvictArgs &a, int row, int n, int n_digits)
+{
+    Known k(a.keep, n);
+    for (int i = 0; i < n_digits && !k.done(); ++i) next_digit(l, a.hist + ((int64_t)row * kDigits + i) * kBins, k);
+    return k;
+}
+
+// Orders and weights of eight slots of a thread, those behind the chunk's end of its last one.
+struct Eight {
+    int32_t o[8];
+    float x[8];
+    __device__ void load(const Row &r, const Chunk &c, const int (&j)[8])
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            o[e] = r.order[min(j[e], c.end - 1)];
+            x[e] = r.w[min(j[e], c.end - 1)];
+        }
+    }
+    __device__ void load_first(const Row &r, const Chunk &c)
+    {
+        int j[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) j[e] = c.begin + e * kChunkThreads + (int)threadIdx.x;
+        load(r, c, j);
+    }
+};
+
+// f(slots, ranks, what was loaded) of eight slots of the chunk at a time; a rank behind the end is not one.  The first eight are there: they are
+// requested before anything else.
+template <typename F>
+__device__ inline void for_ranks(const EvictArgs &a, const Row &r, const Chunk &c, Eight &v, int32_t newest, F f)
+{
+    for_eights<kChunkThreads>(c.begin, c.end, [&](const int (&j)[8]) {
+        if (j[0] != c.begin + (int)threadIdx.x) v.load(r, c, j);
+        uint32_t rank[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rank[e] = rank_of(v.x[e], is_safe(a, v.o[e], newest));
+        f(j, rank, v);
+    });
+}
+
+// Counts of the digit behind those that are known; rows whose last rank is known well enough are left.
+__global__ __launch_bounds__(kChunkThreads) void evict_count(const EvictArgs a, int digit)
+{
+    __shared__ int hist[kBins];
+    __shared__ DigitLds<kChunkThreads> digits;
+    const int row = blockIdx.x, tid = threadIdx.x;
+    const Row r(a, row);
+    const Chunk c(a, r.n);
+    if (r.n <= a.keep || c.begin >= c.end) return;
+    Eight v;
+    v.load_first(r, c);
+    const int32_t newest = newest_of(a, row);
+    for (int i = tid; i < kBins; i += kChunkThreads) hist[i] = 0;
+    const Known k = known_after(digits, a, row, r.n, digit);
+    if (k.done()) return;
+    __syncthreads();
+    for_ranks(a, r, c, v, newest, [&](const int (&j)[8], const uint32_t (&rank)[8], const Eight &) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) count_in(hist, j[e] < c.end && k.candidate(rank[e]), k.bin(rank[e]));
+    });
+    __syncthreads();
+    int *all = a.hist + ((int64_t)row * kDigits + digit) * kBins;
+    for (int i = tid; i < kBins; i += kChunkThreads)
+        if (hist[i] > 0) atomicAdd(&all[i], hist[i]);
+}
+
+// Which slots stay: a bit each, ties apart where only some of them do.
+__global__ __launch_bounds__(kChunkThreads) void evict_mark(const EvictArgs a)
+{
+    __shared__ DigitLds<kChunkThreads> digits;
+    const int row = blockIdx.x;
+    const Row r(a, row);
+    const Chunk c(a, r.n);
+    if (r.n <= a.keep || c.begin >= c.end) return;
+    Eight v;
+    v.load_first(r, c);
+    const int32_t newest = newest_of(a, row);
+    const Known k = known_after(digits, a, row, r.n, kDigits);
+    const bool some = k.in_bin > k.need, out = r.moves_out();
+    int4 counts = make_int4(0, 0, 0, 0);
+    for_ranks(a, r, c, v, newest, [&](const int (&j)[8], const uint32_t (&rank)[8], const Eight &u) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bool has = j[e] < c.end, tie = has && k.candidate(rank[e]), stays = has && (k.larger(rank[e]) || (tie && !some));
+            const uint64_t above = __ballot(stays), ties = some ? __ballot(tie) : 0;
+            if ((threadIdx.x & 63) == 0 && has) {
+                a.above[(int64_t)row * a.words + j[e] / 64] = above;
+                a.ties[(int64_t)row * a.words + j[e] / 64] = ties;
+            }
+            const bool front = j[e] < a.keep;
+            counts.x += stays && front; counts.y += stays && !front;
+            counts.z += some && tie && front; counts.w += some && tie && !front;
+            if (out && stays && front) r.leave(j[e], u.x[e], u.o[e]);
+        }
+    });
+    __shared__ int4 waves[kChunkThreads / 64];
+    counts = make_int4(wave_sum(counts.x), wave_sum(counts.y), wave_sum(counts.z), wave_sum(counts.w));
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = counts;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kChunkThreads / 64; ++w) {
+            counts.x += waves[w].x; counts.y += waves[w].y; counts.z += waves[w].z; counts.w += waves[w].w;
+        }
+        a.marked[(int64_t)row * a.chunks + blockIdx.y] = counts;
+        if (blockIdx.y == 0) a.need[row] = k.need;
+    }
+}
+
+// The chunk's part of the list of a row's moves: a thread counts 64 slots, a wave writes them.  Of the ties the lowest stay.
+__global__ __launch_bounds__(kChunkThreads) void evict_list(const EvictArgs a)
+{
+    __shared__ Sums<kChunkThreads> sums;
+    __shared__ uint64_t lists[kChunkThreads];
+    __shared__ int places[kChunkThreads];
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+    const Row r(a, row);
+    const Chunk c(a, r.n);
+    if (r.n <= a.keep || c.begin >= c.end) return;
+    // what the chunks in front of this one have, and all (a wave has them all: chunks <= 64)
+    const int words = (r.n + 63) / 64, each = (words + a.chunks - 1) / a.chunks * 64;
+    const int begin = min(r.n, lane * each), end = min(r.n, begin + each);
+    const int4 m = lane < a.chunks && begin < end ? a.marked[(int64_t)row * a.chunks + lane] : make_int4(0, 0, 0, 0);
+    const int need = a.need[row], ties = m.z + m.w, kept = max(0, min(ties, need - (wave_upto(ties) - ties))), kept_front = min(kept, m.z);
+    const int holes = min(max(a.keep - begin, 0), end - begin) - m.x - kept_front, late = m.y + kept - kept_front;
+    const int upto = wave_upto(holes + late);
+    const int ties_before = __shfl(wave_upto(ties) - ties, (int)blockIdx.y, 64), list_before = __shfl(upto - holes - late, (int)blockIdx.y, 64);
+    const int all_listed = __shfl(upto, 63, 64);
+    if (blockIdx.y == 0 && tid == 0) a.counts[row] = all_listed / 2;
+
+    const uint64_t *above_words = a.above + (int64_t)row * a.words, *ties_words = a.ties + (int64_t)row * a.words;
+    int32_t *moves = a.moves + (int64_t)row * 2 * a.max_moves;
+    int ties_so_far = ties_before, so_far = list_before, total;
+    for (int w0 = c.begin / 64; w0 * 64 < c.end; w0 += kChunkThreads) {
+        const int word = w0 + tid;
+        const bool has = word * 64 < c.end;
+        uint64_t stays = has ? above_words[word] : 0, tie = has ? ties_words[word] : 0;
+        const int left = need - ties_so_far - sum_before(sums, __popcll(tie), &total);
+        ties_so_far += total;
+        for (int drop = __popcll(tie) - max(left, 0); drop > 0; --drop) tie &= ~(1ull << (63 - __builtin_clzll(tie)));
+        stays |= tie;
+        const int front = has ? min(max(a.keep - word * 64, 0), 64) : 0, in_word = has ? min(r.n - word * 64, 64) : 0;   // slots in front of `keep`, slots
+        const uint64_t in_front = front == 64 ? ~0ull : (1ull << front) - 1, all = in_word == 64 ? ~0ull : (1ull << in_word) - 1;
+        const uint64_t list = ((~stays & in_front) | (stays & ~in_front)) & all;   // evicted in front, kept behind
+        if (r.moves_out())
+            for (tie &= in_front; tie != 0; tie &= tie - 1) {
+                const int j = word * 64 + __builtin_ctzll(tie);
+                r.leave(j, r.w[j], r.order[j]);
+            }
+        lists[tid] = list;
+        places[tid] = so_far + sum_before(sums, __popcll(list), &total);   // (its barriers are behind both)
+        so_far += total;
         __syncthreads();
-        prefix |= (uint32_t)shared_digit << shift;
-        need = shared_need;
+        for (int i = tid >> 6; i < kChunkThreads && (w0 + i) * 64 < c.end; i += kChunkThreads / 64) {
+            const uint64_t x = lists[i];
+            if ((x >> lane) & 1) moves[places[i] + __popcll(x & ((1ull << lane) - 1))] = (w0 + i) * 64 + lane;
+        }
         __syncthreads();
     }
-    // `need` slots of rank `prefix` stay, the lowest ones
-    int32_t *to = a.to + (int64_t)row * a.max_moves, *from = a.from + (int64_t)row * a.max_moves;
-    int ties = 0, holes = 0, late = 0;
-    for (int j0 = 0; j0 < n; j0 += kSelectThreads) {
-        const int j = j0 + tid;
-        const uint32_t r = j < n ? rank(j) : 0;
-        const bool tie = j < n && r == prefix;
-        int total;
-        const int tie_rank = ties + before_in_block(tie, sums, &total);
-        ties += total;
-        const bool kept = j < n && (r > prefix || (tie && tie_rank < need));
-        const bool hole = j < a.keep && !kept, moved = j >= a.keep && kept;
-        const int hole_rank = holes + before_in_block(hole, sums, &total);
-        holes += total;
-        const int late_rank = late + before_in_block(moved, sums, &total);
-        late += total;
-        if (hole) to[hole_rank] = j;
-        if (moved) from[late_rank] = j;
-        if (kept && j < a.keep) {
-            if (w_out != w) w_out[j] = w[j];
-            if (ord_out != ord) ord_out[j] = ord[j];
-        }
-    }
-    if (tid == 0) a.counts[row] = holes;
 }
 
 __device__ inline int64_t slot_offset(const bs_cache &c, int seq, int head, int slot)   // -1: no page
@@ -148,30 +571,54 @@ __device__ inline int64_t slot_offset(const bs_cache &c, int seq, int head, int 
     return page * c.page_stride + head * c.head_stride + (slot % c.page_size) * c.slot_stride;
 }
 
-// A move is done by as many threads as a row has pieces of 16 bytes.
-template <typename T>
-__global__ __launch_bounds__(kMoveThreads) void evict_move(const EvictArgs a)
+// `count` moves, each by as many threads as a row has pieces of 16 bytes.
+template <typename T, typename M>
+__device__ inline void do_moves(const EvictArgs &a, int row, int count, M move)
 {
-    const int row = blockIdx.x, seq = row / a.cache.n_kv_heads, head = row - seq * a.cache.n_kv_heads;
+    const int seq = row / a.cache.n_kv_heads, head = row - seq * a.cache.n_kv_heads;
     constexpr int PER = 16 / sizeof(T);
-    const int pieces = a.cache.head_dim / PER, n = a.counts[row];
+    const unsigned pieces = a.cache.head_dim / PER;
     const T *k = static_cast<const T *>(a.cache.k), *v = static_cast<const T *>(a.cache.v);
-    for (int64_t idx = (int64_t)blockIdx.y * kMoveThreads + threadIdx.x; idx < (int64_t)n * pieces; idx += (int64_t)gridDim.y * kMoveThreads) {
-        const int i = (int)(idx / pieces), p = (int)(idx - (int64_t)i * pieces);
-        const int to = a.to[(int64_t)row * a.max_moves + i], from = a.from[(int64_t)row * a.max_moves + i];
-        const int64_t dst = slot_offset(a.cache, seq, head, to), src = slot_offset(a.cache, seq, head, from);
+    for (unsigned idx = threadIdx.x; idx < count * pieces; idx += kMoveThreads) {
+        const unsigned i = idx / pieces, p = idx - i * pieces;
+        const int2 m = move(i);   // to, from
+        const int64_t dst = slot_offset(a.cache, seq, head, m.x), src = slot_offset(a.cache, seq, head, m.y);
         if (dst >= 0 && src >= 0) {
             const uint4 x = *reinterpret_cast<const uint4 *>(k + src + p * PER), y = *reinterpret_cast<const uint4 *>(v + src + p * PER);
             *reinterpret_cast<uint4 *>(const_cast<T *>(k) + dst + p * PER) = x;
             *reinterpret_cast<uint4 *>(const_cast<T *>(v) + dst + p * PER) = y;
         }
         if (p == 0) {
-            a.weights_out[row * a.out_stride + to] = a.weights[row * a.in_stride + from];
-            a.order_out[row * a.out_stride + to] = a.order[row * a.in_stride + from];
+            a.weights_out[row * a.out_stride + m.x] = a.weights[row * a.in_stride + m.y];
+            a.order_out[row * a.out_stride + m.x] = a.order[row * a.in_stride + m.y];
         }
     }
-    // (the lengths were read by the kernel before)
-    if (blockIdx.y == 0 && head == 0 && threadIdx.x == 0) a.lens_out[seq] = min(used_slots(a, seq), a.keep);
+}
+
+// (the kernels before have read the lengths)
+__device__ inline void set_length(const EvictArgs &a, int row)
+{
+    if (blockIdx.y == 0 && row % a.cache.n_kv_heads == 0 && threadIdx.x == 0) {
+        const int seq = row / a.cache.n_kv_heads;
+        a.lens_out[seq] = min(used_slots(a, seq), a.keep);
+    }
+}
+
+// Moves [first, first + count) of this workgroup.
+__device__ inline int2 own_moves(int n)
+{
+    const int each = (n + (int)gridDim.y - 1) / (int)gridDim.y, first = min(n, (int)blockIdx.y * each);
+    return make_int2(first, min(each, n - first));
+}
+
+template <typename T>
+__global__ __launch_bounds__(kMoveThreads) void evict_move(const EvictArgs a)
+{
+    const int row = blockIdx.x, n = a.counts[row];
+    const int32_t *moves = a.moves + (int64_t)row * 2 * a.max_moves;
+    const int2 own = own_moves(n);
+    do_moves<T>(a, row, own.y, [&](int i) { return make_int2(moves[own.x + i], moves[n + own.x + i]); });
+    set_length(a, row);
 }
 
 int check_evict(const bs_cache *cache, int32_t keep)
@@ -181,8 +628,71 @@ int check_evict(const bs_cache *cache, int32_t keep)
     return BS_OK;
 }
 
-int64_t max_moves(const bs_cache &c, int32_t keep) { return std::max<int64_t>(0, std::min<int64_t>(keep, cache_slots(c) - keep)); }
-int64_t counts_bytes(const bs_cache &c) { return ((int64_t)c.n_seqs * c.n_kv_heads * 4 + 15) / 16 * 16; }
+// How a call is laid out and its workspace.
+struct Plan {
+    int64_t rows, moves;
+    int32_t chunks, words;      // chunks 0: one workgroup per row
+    int64_t at_moves, at_need, at_newest, at_hist, at_above, at_ties, at_marked, bytes;
+};
+
+Plan make_plan(const bs_cache &c, int32_t keep)
+{
+    Plan p{};
+    const int64_t capacity = cache_slots(c);
+    p.rows = (int64_t)c.n_seqs * c.n_kv_heads;
+    p.moves = std::max<int64_t>(0, std::min<int64_t>(keep, capacity - keep));
+    if (capacity > kRanksMax || (p.rows <= 32 && capacity > 4096)) {
+        p.chunks = (int32_t)std::max<int64_t>(1, std::min<int64_t>({64, (capacity + 1023) / 1024, (1024 + p.rows - 1) / p.rows}));
+        p.words = (int32_t)((capacity + 63) / 64);
+    }
+    const auto whole = [](int64_t bytes) { return (bytes + 255) / 256 * 256; };
+    p.at_moves = whole(p.rows * 4);
+    p.at_need = p.at_moves + whole(p.rows * p.moves * 8);
+    p.at_newest = p.at_need + (p.chunks ? whole(p.rows * 4) : 0);
+    p.at_hist = p.at_newest + whole(p.rows * p.chunks * 4);
+    p.at_above = p.at_hist + (p.chunks ? p.rows * kDigits * kBins * 4 : 0);
+    p.at_ties = p.at_above + whole(p.rows * p.words * 8);
+    p.at_marked = p.at_ties + whole(p.rows * p.words * 8);
+    p.bytes = p.at_marked + p.rows * p.chunks * 16;
+    return p;
+}
+
+std::mutex g_mutex;
+bool g_limits[64];   // dynamic LDS of a device's kernels raised
+
+hipError_t device_setup()
+{
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+    std::lock_guard<std::mutex> lock(g_mutex);
+    if (g_limits[dev]) return hipSuccess;
+    const void *const k = reinterpret_cast<const void *>(evict_select<1024, false>);
+    if ((e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kRanksMax * 4)) != hipSuccess) return e;
+    g_limits[dev] = true;
+    return hipSuccess;
+}
+
+hipError_t launch_select(const EvictArgs &a, const Plan &p, hipStream_t st)
+{
+    const int64_t capacity = cache_slots(a.cache);
+    if (p.chunks == 0) {
+        const dim3 grid((unsigned)p.rows);
+        // as few threads as have eight slots each: their barriers are cheaper, and more rows fit a CU
+        if (capacity <= 8 * 256) return launch_kernel(evict_select<256, true>, grid, dim3(256), 0, st, a);
+        if (capacity <= 8 * 512) return launch_kernel(evict_select<512, true>, grid, dim3(512), 0, st, a);
+        if (capacity <= 8 * 1024) return launch_kernel(evict_select<1024, true>, grid, dim3(1024), 0, st, a);
+        if (const hipError_t e = device_setup(); e != hipSuccess) return e;
+        return launch_kernel(evict_select<1024, false>, grid, dim3(1024), (capacity + 1023) / 1024 * 4096, st, a);
+    }
+    const dim3 grid((unsigned)p.rows, (unsigned)p.chunks), block(kChunkThreads);
+    hipError_t e = launch_kernel(evict_newest, grid, block, 0, st, a);
+    for (int digit = 0; digit < kDigits && e == hipSuccess; ++digit) e = launch_kernel(evict_count, grid, block, 0, st, a, digit);
+    if (e == hipSuccess) e = launch_kernel(evict_mark, grid, block, 0, st, a);
+    if (e == hipSuccess) e = launch_kernel(evict_list, grid, block, 0, st, a);
+    return e;
+}
 
 }  // namespace
 }  // namespace bs
@@ -191,7 +701,7 @@ extern "C" int64_t bs_cache_evict_workspace(const bs_cache *cache, int32_t keep)
 {
     using namespace bs;
     if (int rc = check_evict(cache, keep)) return rc;
-    return counts_bytes(*cache) + (int64_t)cache->n_seqs * cache->n_kv_heads * max_moves(*cache, keep) * 8;
+    return make_plan(*cache, keep).bytes;
 }
 
 extern "C" int bs_cache_evict(const bs_cache *cache, const int32_t *lens, int32_t *lens_out, int32_t keep, int32_t keep_first, int32_t keep_last,
@@ -202,7 +712,8 @@ extern "C" int bs_cache_evict(const bs_cache *cache, const int32_t *lens, int32_
     if (!lens || !lens_out || !slots || !slots_out || !workspace || keep_first < 0 || keep_last < 0 || (int64_t)keep_first + keep_last > keep) return BS_EINVAL;
     if (!slots->weights || !slots->order || !slots_out->weights || !slots_out->order) return BS_EINVAL;
     if (check_slots(*cache, slots) || check_slots(*cache, slots_out)) return BS_EINVAL;
-    if ((uintptr_t)workspace % 16 != 0 || workspace_bytes < bs_cache_evict_workspace(cache, keep)) return BS_EINVAL;
+    const Plan p = make_plan(*cache, keep);
+    if ((uintptr_t)workspace % 16 != 0 || workspace_bytes < p.bytes) return BS_EINVAL;
     // the same arrays, or others: in place, rows lie where they lay
     if ((slots->weights == slots_out->weights || slots->order == slots_out->order) && slots->row_stride != slots_out->row_stride) return BS_EINVAL;
     EvictArgs a{};
@@ -212,17 +723,25 @@ extern "C" int bs_cache_evict(const bs_cache *cache, const int32_t *lens, int32_
     a.keep = keep; a.keep_first = keep_first; a.keep_last = keep_last;
     a.weights = slots->weights; a.order = slots->order; a.in_stride = slots->row_stride;
     a.weights_out = slots_out->weights; a.order_out = slots_out->order; a.out_stride = slots_out->row_stride;
-    const int64_t rows = (int64_t)cache->n_seqs * cache->n_kv_heads, moves = max_moves(*cache, keep);
-    a.max_moves = (int32_t)moves;
-    a.counts = static_cast<int32_t *>(workspace);
-    a.to = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + counts_bytes(*cache));
-    a.from = a.to + rows * moves;
+    char *ws = static_cast<char *>(workspace);
+    a.counts = reinterpret_cast<int32_t *>(ws);
+    a.moves = reinterpret_cast<int32_t *>(ws + p.at_moves);
+    a.max_moves = (int32_t)p.moves;
+    a.chunks = p.chunks;
+    a.need = reinterpret_cast<int32_t *>(ws + p.at_need);
+    a.newest = reinterpret_cast<int32_t *>(ws + p.at_newest);
+    a.hist = reinterpret_cast<int32_t *>(ws + p.at_hist);
+    a.above = reinterpret_cast<uint64_t *>(ws + p.at_above);
+    a.ties = reinterpret_cast<uint64_t *>(ws + p.at_ties);
+    a.marked = reinterpret_cast<int4 *>(ws + p.at_marked);
+    a.words = p.words;
     hipStream_t st = (hipStream_t)stream;
-    hipError_t e = launch_kernel(evict_select, dim3((unsigned)rows), dim3(kSelectThreads), 0, st, a);
-    if (e != hipSuccess) return fail_hip(e, "evict_select launch");
+    hipError_t e = launch_select(a, p, st);
+    if (e != hipSuccess) return fail_hip(e, "eviction: select launch");
     const int64_t pieces = (int64_t)cache->head_dim * element_bytes(cache->dtype) / 16;
-    const int64_t blocks = std::max<int64_t>(1, std::min({(moves * pieces + kMoveThreads - 1) / kMoveThreads, (int64_t)1024, (4096 + rows - 1) / rows}));
-    const dim3 grid((unsigned)rows, (unsigned)blocks);
-    e = cache->dtype == BS_BF16 ? launch_kernel(evict_move<__bf16>, grid, dim3(kMoveThreads), 0, st, a) : launch_kernel(evict_move<float>, grid, dim3(kMoveThreads), 0, st, a);
+    const int64_t blocks = std::max<int64_t>(1, std::min({(p.moves * pieces + kMoveThreads - 1) / kMoveThreads, (int64_t)1024, (4096 + p.rows - 1) / p.rows}));
+    const dim3 grid((unsigned)p.rows, (unsigned)blocks);
+    const dim3 block(kMoveThreads);
+    e = cache->dtype == BS_BF16 ? launch_kernel(evict_move<__bf16>, grid, block, 0, st, a) : launch_kernel(evict_move<float>, grid, block, 0, st, a);
     return e == hipSuccess ? BS_OK : fail_hip(e, "evict_move launch");
 }

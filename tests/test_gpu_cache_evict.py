@@ -69,6 +69,15 @@ def test_evict(dtype, hkv, d, page, pool, keep, first, last, in_place):
     run(c, keep, first, last, *draw(c, keep), in_place)
 
 
+@pytest.mark.parametrize("lens", [[6000, 0, 63], [1, 8193, 200, 20000, 5, 777] * 9, [5000, 3, 7000] * 14, [3000, 4000] * 20])
+@pytest.mark.parametrize("keep,first,last", [(1, 0, 1), (200, 4, 196), (1023, 5, 100), (5000, 0, 0)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_rows_of_other_lengths(lens, keep, first, last, in_place):
+    """In chunks; one workgroup each with ranks in LDS; one each with ranks in registers, of 1024 and of 512 threads."""
+    c = Paged("bf16", 1, 8, 16, lens, seed=keep)
+    run(c, keep, first, last, *draw(c, keep), in_place)
+
+
 @pytest.mark.parametrize("n,keep", [(9000, 1000), (9000, 8999), (40000, 8192), (70001, 65536), (140000, 10)])
 def test_long(n, keep):
     c = Paged("bf16", 2, 8, 256, [n, n // 2], seed=1)
@@ -76,8 +85,10 @@ def test_long(n, keep):
 
 
 @pytest.mark.parametrize("values", ["equal", "zeros", "few", "special", "one bit apart"])
-def test_ties_and_special_weights(values):
-    c = Paged("bf16", 2, 8, 16, [700, 3000], seed=2)
+@pytest.mark.parametrize("capacity", [3008, 6000, 40000])   # few rows: one workgroup each, or in chunks
+def test_ties_and_special_weights(values, capacity):
+    make = lambda: Paged("bf16", 2, 8, 16, [700, 3000], capacity=capacity, seed=2)
+    c = make()
     w, order = draw(c, 5)
     rng = np.random.default_rng(6)
     if values == "equal":
@@ -92,11 +103,12 @@ def test_ties_and_special_weights(values):
     else:
         w = (np.full(w.shape, 0x3f800000, dtype=np.int32) + rng.integers(0, 5, w.shape, dtype=np.int32)).view(np.float32)
     for keep in (1, 350, 699, 2999):
-        run(Paged("bf16", 2, 8, 16, [700, 3000], seed=2), keep, 0, 0, w, order, False)
+        run(make(), keep, 0, 0, w, order, False)
 
 
-def test_orders_that_an_eviction_mixed():
-    c = Paged("bf16", 2, 64, 16, [500, 900], seed=3)
+@pytest.mark.parametrize("capacity", [1008, 5000])
+def test_orders_that_an_eviction_mixed(capacity):
+    c = Paged("bf16", 2, 64, 16, [500, 900], capacity=capacity, seed=3)
     w, order = draw(c, 7)
     rng = np.random.default_rng(8)
     for s, n in enumerate((500, 900)):
