@@ -28,7 +28,9 @@ namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
-struct Share { int32_t item, last; };   // of a workgroup: the item that begins in its share and goes on behind it (-1: none), and the last workgroup that has a part of it
+// An item in more than one share: the first and the last workgroup that have a part of it.  Filed under the item where there are fewer items than shares
+// (first = last: a whole one), else under the first share (item -1: none goes on behind it).
+struct Cut { int32_t item, first, last; };
 
 struct DecodeArgs {
     bs_cache cache;
@@ -42,9 +44,11 @@ struct DecodeArgs {
     float scale_log2e;
     float *part_o;                // [2 n_shares][rows][d]: of share w, 2 w the item that began before it, 2 w + 1 the one that goes on behind it
     float2 *part_ml;              // reference point and sum
-    Share *shares;
+    Cut *cuts;
+    int32_t by_item;
     // with weights
-    float *scores;                // [block][rows][slots of a block], times scale log2(e)
+    int32_t item_blocks;          // room for the blocks of an item
+    float *scores;                // [seq][item][block][rows][slots of a block], times scale log2(e)
     float *log_sums;              // [seq][query head], to base 2
     const float *weights;
     float *weights_out;
@@ -68,8 +72,12 @@ struct Traits {
     __device__ static int swizzle(int r) { return kRowBytes == 128 ? (r >> 1) & 7 : r & 15; }
 };
 
-// Blocks of a sequence that are visible, from block `first` on.
-struct Visible { int n, begin, first, blocks; };
+// Beginning an item (its query rows, an empty pipeline, the merge of the waves) costs about as much as so many blocks: shares are equal with
+// that counted.  Else a share of many short sequences takes longest: 48 sequences of 17 to 16K slots 100 us, 123 without.
+constexpr int kItemBlocks = 4;
+
+// Blocks of a sequence that are visible, from block `first` on; `units`: those of an item and what its beginning costs.
+struct Visible { int n, begin, first, blocks, units; };
 template <int KEYS>
 __device__ inline Visible visible(const DecodeArgs &a, int seq)
 {
@@ -78,14 +86,15 @@ __device__ inline Visible visible(const DecodeArgs &a, int seq)
     v.begin = a.window > 0 ? max(0, v.n - a.window) : 0;
     v.first = v.begin / KEYS;
     v.blocks = (v.n + KEYS - 1) / KEYS - v.first;
+    v.units = v.blocks > 0 ? v.blocks + kItemBlocks : 0;
     return v;
 }
 
-// The share of this workgroup in the row of all blocks: items of a sequence one behind the other, sequences one behind the other.
-struct Place { int seq, item, block; };   // sequence, item of it, block of that
-struct Range { int begin, end; Place at; int each; };   // `each`: blocks of a share
+// The share of this workgroup in the row of all units: items of a sequence one behind the other, sequences one behind the other.
+struct Place { int seq, item, unit; };   // sequence, item of it, unit of that
+struct Range { int begin, end; Place at; int each; };   // `each`: units of a share
 
-// `items` per sequence.  All threads of the workgroup; blocks of a share: a multiple of four.
+// `items` per sequence.  All threads of the workgroup; units of a share: a multiple of four, for the four waves.
 template <int KEYS>
 __device__ inline Range own_range(const DecodeArgs &a, int items, int share, int n_shares)
 {
@@ -95,23 +104,23 @@ __device__ inline Range own_range(const DecodeArgs &a, int items, int share, int
     int total;
     if (S == 1) {
         const Visible v = visible<KEYS>(a, 0);
-        total = v.blocks * items;
+        total = v.units * items;
         r.each = max(kWaves, ((total + n_shares - 1) / n_shares + kWaves - 1) / kWaves * kWaves);
         r.begin = (int)min((int64_t)total, (int64_t)share * r.each);
         r.end = min(total, r.begin + r.each);
         r.at.seq = 0;
-        r.at.item = v.blocks > 0 ? r.begin / v.blocks : 0;
-        r.at.block = r.begin - r.at.item * v.blocks;
+        r.at.item = v.units > 0 ? r.begin / v.units : 0;
+        r.at.unit = r.begin - r.at.item * v.units;
         return r;
     }
     // a thread adds up a few sequences one behind the other
     const int each = (S + kThreads - 1) / kThreads, s0 = min(S, tid * each), s1 = min(S, s0 + each);
-    const auto blocks_of = [&](int s) {
+    const auto units_of = [&](int s) {
         const int n = max(0, min(a.lens[s], a.cache.max_pages * a.cache.page_size)), begin = a.window > 0 ? max(0, n - a.window) : 0;
-        return ((n + KEYS - 1) / KEYS - begin / KEYS) * items;
+        return n > 0 ? ((n + KEYS - 1) / KEYS - begin / KEYS + kItemBlocks) * items : 0;
     };
     int mine = 0;
-    for (int s = s0; s < s1; ++s) mine += blocks_of(s);
+    for (int s = s0; s < s1; ++s) mine += units_of(s);
     int upto = mine;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -131,17 +140,17 @@ __device__ inline Range own_range(const DecodeArgs &a, int items, int share, int
     r.begin = (int)min((int64_t)total, (int64_t)share * r.each);
     r.end = min(total, r.begin + r.each);
     if (r.begin >= before && r.begin < before + mine) {
-        int left = r.begin - before, s = s0, n = blocks_of(s0);
-        while (left >= n) { left -= n; n = blocks_of(++s); }
-        const int blocks = n / items;
+        int left = r.begin - before, s = s0, n = units_of(s0);
+        while (left >= n) { left -= n; n = units_of(++s); }
+        const int units = n / items;
         found[0] = s;
-        found[1] = left / blocks;
-        found[2] = left - left / blocks * blocks;
+        found[1] = left / units;
+        found[2] = left - left / units * units;
     }
     __syncthreads();
     r.at.seq = __builtin_amdgcn_readfirstlane(found[0]);
     r.at.item = __builtin_amdgcn_readfirstlane(found[1]);
-    r.at.block = __builtin_amdgcn_readfirstlane(found[2]);
+    r.at.unit = __builtin_amdgcn_readfirstlane(found[2]);
     r.begin = __builtin_amdgcn_readfirstlane(r.begin);
     r.end = __builtin_amdgcn_readfirstlane(r.end);
     r.each = __builtin_amdgcn_readfirstlane(r.each);
@@ -189,7 +198,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void decode_shares(const
                 store_row4(static_cast<T *>(a.out) + s * a.out_seq + (i / CH4) * a.out_head + i % CH4 * 4, make_float4(0.f, 0.f, 0.f, 0.f));
 
     const Range range = own_range<KEYS>(a, items, blockIdx.x, gridDim.x);
-    if (tid == 0) a.shares[blockIdx.x] = Share{-1, 0};
+    if (tid == 0 && !a.by_item) a.cuts[blockIdx.x].item = -1;
     if (range.begin >= range.end) return;
 
     typedef __attribute__((address_space(3))) void *lds_ptr;
@@ -232,15 +241,17 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void decode_shares(const
     int pos = range.begin;
     Visible vis = visible<KEYS>(a, at.seq);
     while (pos < range.end) {
-        while (at.item == items || vis.blocks == 0) {   // the next sequence that has some
+        while (at.item == items || vis.units == 0) {   // the next sequence that has some
             at.item = 0;
             vis = visible<KEYS>(a, ++at.seq);
         }
-        const int blocks = min(vis.blocks - at.block, range.end - pos);
+        const int block = max(0, at.unit - kItemBlocks);   // the first one
+        const int blocks = min(vis.blocks - block, range.end - pos - max(0, kItemBlocks - at.unit));
+        if (blocks <= 0) break;   // the share ends where the item begins
         const int kvh = at.item / a.groups, row0 = kvh * a.G + (at.item - kvh * a.groups) * 32;
         const int n_rows = min(ROWS, (kvh + 1) * a.G - row0);
         const int n_steps = blocks > wave ? (blocks - wave + kWaves - 1) / kWaves : 0;
-        const int b0 = vis.first + at.block + wave;   // step i: block b0 + 4 i of the sequence
+        const int b0 = vis.first + block + wave;   // step i: block b0 + 4 i of the sequence
 
         // Page numbers of 16 slots each; which slots of a block have a page.
         const int32_t *table = a.cache.page_table + (int64_t)at.seq * a.cache.max_pages;
@@ -332,6 +343,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void decode_shares(const
                 for (int i = 0; i < 4; ++i) o[rb][nb][i] = 0.f;
         }
 
+        float *scores = WEIGHTS ? a.scores + (((int64_t)at.seq * items + at.item) * a.item_blocks + b0) * a.rows * KEYS : nullptr;   // (no window: vis.first = 0)
         uint32_t there0 = s0.there, there1 = s1.there;   // of this block, of the next one
         for (int i = 0; i < n_steps; ++i) {
             const int stage = (i & 1) * 2 * BLK;
@@ -390,7 +402,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void decode_shares(const
                     }
                 if constexpr (WEIGHTS) {
                     if (rb * 16 + col < n_rows) {
-                        float *to = a.scores + ((int64_t)(pos + wave + kWaves * i) * a.rows + rb * 16 + col) * KEYS + 4 * grp;
+                        float *to = scores + ((int64_t)(kWaves * i) * a.rows + rb * 16 + col) * KEYS + 4 * grp;
 #pragma unroll
                         for (int h = 0; h < SUB; ++h)
                             *reinterpret_cast<float4 *>(to + 16 * h) = make_float4(s[rb][h][0] * c, s[rb][h][1] * c, s[rb][h][2] * c, s[rb][h][3] * c);
@@ -493,7 +505,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void decode_shares(const
             }
         }
         __syncthreads();
-        const bool begins = at.block == 0, ends = at.block + blocks == vis.blocks;
+        const bool begins = block == 0, ends = block + blocks == vis.blocks;
         const int64_t slot = (int64_t)(2 * blockIdx.x + (begins ? 1 : 0)) * a.rows;
         for (int idx = tid; idx < n_rows * CH4; idx += kThreads) {
             const int row = idx / CH4, ch = idx % CH4;
@@ -522,16 +534,19 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void decode_shares(const
                 if (ch == 0) a.part_ml[slot + row] = make_float2(m, l);
             }
         }
-        if (begins && !ends && tid == 0) a.shares[blockIdx.x] = Share{at.seq * items + at.item, (pos + vis.blocks - 1) / range.each};
-        pos += blocks;
-        at.block = 0;
+        if (begins && tid == 0 && (a.by_item || !ends)) {
+            const int item = at.seq * items + at.item;
+            a.cuts[a.by_item ? item : (int)blockIdx.x] = Cut{item, (int)blockIdx.x, (pos - at.unit + vis.units - 1) / range.each};
+        }
+        pos += vis.units - at.unit;   // (behind the share's end if the item is cut)
+        at.unit = 0;
         ++at.item;
         if (pos < range.end) __syncthreads();   // the ring is free again
     }
 }
 
-// Joins the parts of the item that begins in share blockIdx.x and goes on behind it, row blockIdx.y: threads are D / 4 channel quads
-// times the parts side by side, in a fixed order.
+// Joins the parts of a row (blockIdx.y) of an item that was cut (blockIdx.x): threads are D / 4 channel quads times the parts side by side, in a
+// fixed order.
 template <typename T, int D, bool WEIGHTS>
 __global__ __launch_bounds__(256) void decode_join(const DecodeArgs a)
 {
@@ -539,22 +554,39 @@ __global__ __launch_bounds__(256) void decode_join(const DecodeArgs a)
     __shared__ float4 acc[LANES][CH4];
     __shared__ float2 ml[LANES];
     const int tid = threadIdx.x, ch = tid % CH4, p0 = tid / CH4, row = blockIdx.y;
-    const Share share = a.shares[blockIdx.x];
-    if (share.item < 0) return;
-    const int items = a.cache.n_kv_heads * a.groups, seq = share.item / items, item = share.item - seq * items;
+    const int items = a.cache.n_kv_heads * a.groups;
+    if (a.by_item && a.lens[blockIdx.x / items] <= 0) return;   // (nobody had it)
+    const Cut cut = a.cuts[blockIdx.x];
+    if (a.by_item ? cut.first == cut.last : cut.item < 0) return;
+    const int seq = cut.item / items, item = cut.item - seq * items;
     const int kvh = item / a.groups, row0 = kvh * a.G + (item - kvh * a.groups) * 32;
     if (row >= min(a.rows, (kvh + 1) * a.G - row0)) return;
     float m = -INFINITY, l = 0.f;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int w = (int)blockIdx.x + p0; w <= share.last; w += LANES) {
-        const int64_t at = (int64_t)(2 * w + (w == (int)blockIdx.x ? 1 : 0)) * a.rows + row;
-        const float2 x = a.part_ml[at];
-        const float4 y = *reinterpret_cast<const float4 *>(a.part_o + at * D + 4 * ch);
-        const float m_new = fmaxf(m, x.x);
-        const float f0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * a.scale_log2e), f1 = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x.x - m_new) * a.scale_log2e);
-        l = l * f0 + x.y * f1;
-        sum.x = sum.x * f0 + y.x * f1; sum.y = sum.y * f0 + y.y * f1; sum.z = sum.z * f0 + y.z * f1; sum.w = sum.w * f0 + y.w * f1;
-        m = m_new;
+    // loads of eight parts go out together ; those behind the last one to that one
+    for (int w0 = cut.first + p0; w0 <= cut.last; w0 += 8 * LANES) {
+        float2 x[8];
+        float4 y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int w = min(w0 + i * LANES, cut.last);
+            const int64_t at = (int64_t)(2 * w + (w == cut.first ? 1 : 0)) * a.rows + row;
+            x[i] = a.part_ml[at];
+            y[i] = *reinterpret_cast<const float4 *>(a.part_o + at * D + 4 * ch);
+        }
+        const float m_old = m;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, x[i].x);
+        const float old = m_old == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_old - m) * a.scale_log2e);
+        l *= old;
+        sum.x *= old; sum.y *= old; sum.z *= old; sum.w *= old;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (w0 + i * LANES > cut.last) continue;
+            const float f = x[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[i].x - m) * a.scale_log2e);
+            l = fmaf(x[i].y, f, l);
+            sum.x = fmaf(y[i].x, f, sum.x); sum.y = fmaf(y[i].y, f, sum.y); sum.z = fmaf(y[i].z, f, sum.z); sum.w = fmaf(y[i].w, f, sum.w);
+        }
     }
     acc[p0][ch] = sum;
     if (ch == 0) ml[p0] = make_float2(m, l);
@@ -586,30 +618,41 @@ __global__ __launch_bounds__(kThreads) void decode_weights(const DecodeArgs a)
     int pos = range.begin;
     if (pos >= range.end) return;
     Visible vis = visible<KEYS>(a, at.seq);
-    // where the sequence's blocks begin among those of all items
-    int64_t before = (int64_t)(pos - at.item * vis.blocks - at.block) * a.groups;
     while (pos < range.end) {
-        while (at.item == n_kv || vis.blocks == 0) {
-            before += (int64_t)vis.blocks * n_kv * a.groups;
+        while (at.item == n_kv || vis.units == 0) {
             at.item = 0;
             vis = visible<KEYS>(a, ++at.seq);
         }
-        const int blocks = min(vis.blocks - at.block, range.end - pos);
+        const int block = max(0, at.unit - kItemBlocks);
+        const int blocks = min(vis.blocks - block, range.end - pos - max(0, kItemBlocks - at.unit));
+        if (blocks <= 0) break;
         const int64_t row = (int64_t)at.seq * n_kv + at.item;
         const float *logs = a.log_sums + row * a.G;
-        for (int b = side; b < blocks; b += kSide) {
-            const int j = (at.block + b) * KEYS + key;
-            if (j >= vis.n) continue;
-            float sum = 0.f;
-            for (int g = 0; g < a.groups; ++g) {
-                const float *x = a.scores + (before + ((int64_t)at.item * a.groups + g) * vis.blocks + at.block + b) * a.rows * KEYS + key;
-                const int n_rows = min(a.rows, a.G - 32 * g);
-                for (int r = 0; r < n_rows; ++r) sum += __builtin_amdgcn_exp2f(x[r * KEYS] - logs[32 * g + r]);
+        // loads of four slots of a thread go out together, those behind the last one to that one
+        for (int b = block + side; b < block + blocks; b += 4 * kSide) {
+            int j[4];
+            float sum[4], w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                j[i] = min((b + i * kSide) * KEYS + key, vis.n - 1);
+                sum[i] = 0.f;
+                w[i] = a.weights[row * a.in_stride + j[i]];
             }
-            a.weights_out[row * a.out_stride + j] = a.weights[row * a.in_stride + j] + sum;
+            for (int g = 0; g < a.groups; ++g) {
+                const float *x = a.scores + (row * a.groups + g) * a.item_blocks * a.rows * KEYS;
+                const int n_rows = min(a.rows, a.G - 32 * g);
+                for (int r = 0; r < n_rows; ++r) {
+                    const float log_sum = logs[32 * g + r];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[i] += __builtin_amdgcn_exp2f(x[((int64_t)(j[i] / KEYS) * a.rows + r) * KEYS + j[i] % KEYS] - log_sum);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (b + i * kSide < block + blocks && (b + i * kSide) * KEYS + key < vis.n) a.weights_out[row * a.out_stride + j[i]] = w[i] + sum[i];
         }
-        pos += blocks;
-        at.block = 0;
+        pos += vis.units - at.unit;
+        at.unit = 0;
         ++at.item;
     }
 }
@@ -663,8 +706,9 @@ int check_decode(const bs_cache *cache, int32_t n_q_heads)
 // How a call is laid out over the chip and its workspace.
 struct Plan {
     int32_t groups, row_blocks, rows, n_shares;
-    int64_t blocks;                                         // at most
-    int64_t part_o, part_ml, shares, scores, log_sums, bytes;   // offsets
+    int64_t per_item, blocks;                               // at most
+    int64_t part_o, part_ml, cuts, scores, log_sums, bytes;   // offsets
+    int32_t n_cuts;                                         // entries of them
 };
 
 // Nothing but sizes, so that a graph of a call stays right when lengths change.
@@ -674,15 +718,17 @@ int make_plan(const bs_cache &c, int32_t n_q_heads, bool weights, int n_cus, Pla
     p->groups = (G + 31) / 32;
     p->row_blocks = G > 16 ? 2 : 1;
     p->rows = std::min(G, 32);
-    const int64_t per_item = (cache_slots(c) + keys - 1) / keys + 1;   // (a window may begin and end inside a block)
-    if ((int64_t)c.n_seqs * c.n_kv_heads > INT32_MAX / p->groups || (int64_t)c.n_seqs * c.n_kv_heads * p->groups > INT32_MAX / 2 / per_item) return BS_EUNSUPPORTED;
-    p->blocks = (int64_t)c.n_seqs * c.n_kv_heads * p->groups * per_item;
+    p->per_item = (cache_slots(c) + keys - 1) / keys + 1;   // (a window may begin and end inside a block)
+    const int64_t units = p->per_item + kItemBlocks;
+    if ((int64_t)c.n_seqs * c.n_kv_heads > INT32_MAX / p->groups || (int64_t)c.n_seqs * c.n_kv_heads * p->groups > INT32_MAX / 2 / units) return BS_EUNSUPPORTED;
+    p->blocks = (int64_t)c.n_seqs * c.n_kv_heads * p->groups * p->per_item;
     p->n_shares = (int32_t)std::min<int64_t>((int64_t)n_cus * (c.head_dim == 64 ? 2 : 1), (p->blocks + kWaves - 1) / kWaves);
     const auto whole = [](int64_t bytes) { return (bytes + 255) / 256 * 256; };
     p->part_o = 0;
     p->part_ml = whole((int64_t)2 * p->n_shares * p->rows * c.head_dim * 4);
-    p->shares = p->part_ml + whole((int64_t)2 * p->n_shares * p->rows * 8);
-    p->scores = p->shares + whole((int64_t)p->n_shares * sizeof(Share));
+    p->n_cuts = (int32_t)std::min<int64_t>(p->n_shares, (int64_t)c.n_seqs * c.n_kv_heads * p->groups);
+    p->cuts = p->part_ml + whole((int64_t)2 * p->n_shares * p->rows * 8);
+    p->scores = p->cuts + whole((int64_t)p->n_cuts * sizeof(Cut));
     p->log_sums = p->scores + (weights ? whole(p->blocks * p->rows * keys * 4) : 0);
     p->bytes = p->log_sums + (weights ? whole((int64_t)c.n_seqs * n_q_heads * 4) : 0);
     return BS_OK;
@@ -695,7 +741,7 @@ int launch(const DecodeArgs &a, const Plan &p, int n_cus, hipStream_t st)
     hipError_t e = p.row_blocks == 1 ? launch_kernel(decode_shares<T, D, 1, WEIGHTS>, grid, block, Traits<T, D>::kLds, st, a)
                                      : launch_kernel(decode_shares<T, D, 2, WEIGHTS>, grid, block, Traits<T, D>::kLds, st, a);
     if (e != hipSuccess) return fail_hip(e, "decode_shares launch");
-    if (p.n_shares > 1) e = launch_kernel(decode_join<T, D, WEIGHTS>, dim3((unsigned)p.n_shares, (unsigned)p.rows), dim3(256), 0, st, a);
+    if (p.n_shares > 1) e = launch_kernel(decode_join<T, D, WEIGHTS>, dim3((unsigned)p.n_cuts, (unsigned)p.rows), dim3(256), 0, st, a);
     if (e != hipSuccess) return fail_hip(e, "decode_join launch");
     if constexpr (WEIGHTS) {
         const int64_t wgs = std::min<int64_t>((int64_t)n_cus * 8, (p.blocks / p.groups + 3) / 4);
@@ -758,8 +804,10 @@ extern "C" int bs_attn_decode(const bs_cache *cache, const bs_heads *q, const bs
     char *ws = static_cast<char *>(workspace);
     a.part_o = reinterpret_cast<float *>(ws + p.part_o);
     a.part_ml = reinterpret_cast<float2 *>(ws + p.part_ml);
-    a.shares = reinterpret_cast<Share *>(ws + p.shares);
+    a.cuts = reinterpret_cast<Cut *>(ws + p.cuts);
+    a.by_item = p.n_cuts < p.n_shares;
     if (slots) {
+        a.item_blocks = (int32_t)p.per_item;
         a.scores = reinterpret_cast<float *>(ws + p.scores);
         a.log_sums = reinterpret_cast<float *>(ws + p.log_sums);
         a.weights = slots->weights; a.in_stride = slots->row_stride;
