@@ -32,8 +32,9 @@ struct EvictArgs {
     int32_t *order_out;
     int64_t in_stride, out_stride;
     int32_t *counts;            // moves of each row
-    int32_t *moves;             // [row][2 max_moves]: the slots moved into, then those they come from
+    int32_t *moves;             // [row][2 max_moves]: the slots moved into from the front, those they come from up to the end
     int32_t max_moves;
+    int32_t at_once;            // the workgroup that selects moves as well
     // rows in chunks
     int32_t chunks;
     int32_t *need;              // of each row, how many ties stay
@@ -75,15 +76,15 @@ struct Row {
     }
 };
 
-// f(slots of eight of them) for the thread's slots from `begin` on, THREADS apart: loads of eight slots go out together, those behind the end
-// to the last slot.
-template <int THREADS, typename F>
-__device__ inline void for_eights(int begin, int end, F f)
+// f(slots of N of them) for the thread's slots from `begin` on, THREADS apart: loads of N slots go out together, those behind the end to the
+// last slot.
+template <int THREADS, int N, typename F>
+__device__ inline void for_some(int begin, int end, F f)
 {
-    for (int j0 = begin; j0 < end; j0 += 8 * THREADS) {   // (uniform: `begin` is)
-        int j[8];
+    for (int j0 = begin; j0 < end; j0 += N * THREADS) {   // (uniform: `begin` is)
+        int j[N];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) j[e] = j0 + e * THREADS + (int)threadIdx.x;
+        for (int e = 0; e < N; ++e) j[e] = j0 + e * THREADS + (int)threadIdx.x;
         f(j);
     }
 }
@@ -213,16 +214,70 @@ __device__ inline bool is_safe(const EvictArgs &a, int32_t order, int32_t newest
     return order < a.keep_first || (int64_t)order > (int64_t)newest - a.keep_last;
 }
 
+__device__ inline int64_t slot_offset(const bs_cache &c, int seq, int head, int slot)   // in elements; -1: no page
+{
+    const int page = c.page_table[(int64_t)seq * c.max_pages + slot / c.page_size];
+    if (page < 0 || page >= c.n_pages) return -1;
+    return page * c.page_stride + head * c.head_stride + (slot % c.page_size) * c.slot_stride;
+}
+
+typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+
+constexpr int kMovesAtOnce = 256;
+
+// The `n` moves of a row, at most kMovesAtOnce, by one workgroup: where they go from and to, a thread each, then the rows, 16 bytes a thread and
+// four of them under way.
+template <int THREADS>
+__device__ inline void do_moves(const EvictArgs &a, int row, unsigned n)
+{
+    __shared__ int64_t to[kMovesAtOnce], from[kMovesAtOnce];   // in bytes; to = -1: nothing to copy
+    const int seq = row / a.cache.n_kv_heads, head = row - seq * a.cache.n_kv_heads, tid = threadIdx.x;
+    const int bytes = a.cache.dtype == BS_BF16 ? 2 : 4;
+    const unsigned pieces = a.cache.head_dim * bytes / 16, all = n * pieces;
+    const int32_t *moves = a.moves + (int64_t)row * 2 * a.max_moves;
+    char *k = static_cast<char *>(a.cache.k), *v = static_cast<char *>(a.cache.v);
+    if (tid < (int)n) {
+        const int dst = moves[tid], src = moves[2 * a.max_moves - (int)n + tid];
+        const float w = a.weights[row * a.in_stride + src];
+        const int32_t o = a.order[row * a.in_stride + src];
+        const int64_t d = slot_offset(a.cache, seq, head, dst), s = slot_offset(a.cache, seq, head, src);
+        to[tid] = d < 0 || s < 0 ? -1 : d * bytes;
+        from[tid] = s * bytes;
+        a.weights_out[row * a.out_stride + dst] = w;
+        a.order_out[row * a.out_stride + dst] = o;
+    }
+    __syncthreads();
+    for (unsigned idx0 = tid; idx0 < all; idx0 += 4 * THREADS) {
+        uintx4 x[4], y[4];
+        int64_t at[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const unsigned idx = min(idx0 + u * THREADS, all - 1), i = idx / pieces, p = idx - i * pieces;   // (behind the last one: that again)
+            const int64_t dst = to[i];
+            at[u] = dst < 0 ? -1 : dst + 16 * p;
+            x[u] = *reinterpret_cast<const uintx4 *>(k + (dst < 0 ? 0 : from[i] + 16 * p));
+            y[u] = *reinterpret_cast<const uintx4 *>(v + (dst < 0 ? 0 : from[i] + 16 * p));
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (at[u] >= 0) {
+                *reinterpret_cast<uintx4 *>(k + at[u]) = x[u];
+                *reinterpret_cast<uintx4 *>(v + at[u]) = y[u];
+            }
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------------ one workgroup per row
 
 constexpr int kRanksMax = 32768;   // 128 KB of LDS
 
-// SHORT: a thread has at most eight slots and keeps them in registers.  Else ranks lie in LDS, and orders and weights are read again.
-template <int THREADS, bool SHORT>
-// (two rows of 1024 threads share a CU)
-__global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void evict_select(const EvictArgs a)
+// SLOTS > 0: a thread has at most so many slots and keeps them in registers.  Else ranks lie in LDS, and orders and weights are read again.
+template <int THREADS, int SLOTS>
+__global__ __launch_bounds__(THREADS, 4) void evict_select(const EvictArgs a)
 {
-    constexpr int kFlags = (SHORT ? 8 * THREADS : kRanksMax) / 64;
+    constexpr bool SHORT = SLOTS > 0;
+    constexpr int N = SHORT ? SLOTS : 8, kFlags = (SHORT ? SLOTS * THREADS : kRanksMax) / 64;
     __shared__ int hist[kDigits * kBins];
     __shared__ DigitLds<THREADS> digits;
     __shared__ Sums<THREADS> sums;
@@ -237,12 +292,12 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void evict_select
         if (tid == 0) a.counts[row] = 0;
         return;
     }
-    uint32_t rank[8];
-    int32_t o[8];
-    float x[8];
-    const auto load = [&](const int (&j)[8]) __attribute__((always_inline)) {
+    uint32_t rank[N];
+    int32_t o[N];
+    float x[N];
+    const auto load = [&](const int (&j)[N]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < N; ++e) {
             o[e] = r.order[min(j[e], n - 1)];
             x[e] = r.w[min(j[e], n - 1)];
         }
@@ -251,7 +306,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void evict_select
     const auto for_slots = [&](auto f) __attribute__((always_inline)) {
         if constexpr (SHORT) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
+            for (int e = 0; e < N; ++e)
                 if (e * THREADS < n) f(e * THREADS + tid, rank[e]);
         } else {
             for (int j0 = 0; j0 < n; j0 += THREADS) f(j0 + tid, ranks[j0 + tid]);   // (there is room for whole rounds)
@@ -259,10 +314,10 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void evict_select
     };
     if (tid == 0) newest_lds = INT32_MIN;
     int newest = INT32_MIN;
-    for_eights<THREADS>(0, n, [&](const int (&j)[8]) {
+    for_some<THREADS, N>(0, n, [&](const int (&j)[N]) {
         load(j);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < N; ++e) {
             newest = max(newest, o[e]);
             if constexpr (!SHORT) { if (j[e] < n) ranks[j[e]] = rank_of(x[e], false); }
         }
@@ -275,13 +330,13 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void evict_select
     newest = newest_lds;
     if constexpr (SHORT) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) rank[e] = rank_of(x[e], is_safe(a, o[e], newest));
+        for (int e = 0; e < N; ++e) rank[e] = rank_of(x[e], is_safe(a, o[e], newest));
     } else {
-        for_eights<THREADS>(0, n, [&](const int (&j)[8]) {   // (a thread's own slots)
+        for_some<THREADS, N>(0, n, [&](const int (&j)[N]) {   // (a thread's own slots)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = r.order[min(j[e], n - 1)];
+            for (int e = 0; e < N; ++e) o[e] = r.order[min(j[e], n - 1)];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
+            for (int e = 0; e < N; ++e)
                 if (j[e] < n && is_safe(a, o[e], newest)) ranks[j[e]] = ~0u;
         });
     }
@@ -292,17 +347,16 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void evict_select
         next_digit(digits, hist + digit * kBins, known);
     }
 
-    // How many slots with a flag lie before each 64 of them: counts, then their sum in the order of slots.
-    int total;
-    const auto count_flags = [&](auto flag) __attribute__((always_inline)) {
-        for_slots([&](int j, uint32_t &u) {
-            const uint64_t b = __ballot(flag(j, u));
-            if (lane == 0 && j < n) flags[j / 64] = __popcll(b);
-        });
-        __syncthreads();
+    // How many ties (low half) and how many larger ones lie before each 64 slots: counts, then their sum in the order of slots.
+    for_slots([&](int j, uint32_t &u) {
+        const uint64_t tie = __ballot(j < n && known.candidate(u)), larger = __ballot(j < n && known.larger(u));
+        if (lane == 0 && j < n) flags[j / 64] = __popcll(larger) << 16 | __popcll(tie);
+    });
+    __syncthreads();
+    {
         constexpr int EACH = (kFlags + THREADS - 1) / THREADS;
         const int entries = (n + 63) / 64;
-        int mine = 0, c[EACH];
+        int mine = 0, c[EACH], total;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             c[i] = tid * EACH + i < entries ? flags[tid * EACH + i] : 0;
@@ -314,44 +368,42 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void evict_select
             if (tid * EACH + i < entries) flags[tid * EACH + i] = before;
             before += c[i];
         }
-        __syncthreads();
-    };
-    const auto flags_before = [&](int j, bool flag) {
-        const uint64_t b = __ballot(flag);
-        return flags[min(j, n - 1) / 64] + __popcll(b & ((1ull << lane) - 1));
-    };
-    // Of equal ranks the lowest slots stay.  From here on all that matters of a rank is whether its slot stays.
-    const bool ties = known.in_bin > known.need;
-    if (ties) count_flags([&](int j, uint32_t u) { return j < n && known.candidate(u); });
-    for_slots([&](int j, uint32_t &u) {
-        const bool tie = j < n && known.candidate(u);
-        bool stays = tie;
-        if (ties) {
-            const int before = flags_before(j, tie);
-            stays = tie && before < known.need;
-        }
-        u = j < n && (stays || known.larger(u));
-    });
+    }
     __syncthreads();
-    // Holes (evicted in front) and slots that move (kept behind) in one list: as many of the one as of the other.
-    const auto listed = [&](int j, uint32_t stays) { return j < n && (j < a.keep) == (stays == 0); };
-    count_flags(listed);
+    // Of equal ranks the lowest slots stay.  A hole in front is on the list behind as many as were evicted before it, a slot that moves in front of as
+    // many as are kept behind it.
     int32_t *moves = a.moves + (int64_t)row * 2 * a.max_moves;
     for_slots([&](int j, uint32_t &u) {
-        const bool in_list = listed(j, u);
-        const int at = flags_before(j, in_list);
-        if (in_list) moves[at] = j;
+        const bool tie = j < n && known.candidate(u), more = j < n && known.larger(u);
+        const uint64_t below = (1ull << lane) - 1, all_ties = __ballot(tie), all_more = __ballot(more);
+        const uint32_t before = flags[min(j, n - 1) / 64];
+        const int ties = (int)(before & 0xffffu) + __popcll(all_ties & below), kept = (int)(before >> 16) + __popcll(all_more & below) + min(ties, known.need);
+        const bool stays = more || (tie && ties < known.need);
+        if (j < a.keep && !stays) moves[j - kept] = j;
+        if (j < n && j >= a.keep && stays) moves[2 * a.max_moves - a.keep + kept] = j;
+        if (j == a.keep - 1) digits.need[0] = a.keep - kept - stays;   // how many
+        if (j < n) u = stays;   // all that matters from here on
     });
-    if (tid == 0) a.counts[row] = total / 2;
+    __syncthreads();
+    const int n_moves = digits.need[0];
     if (r.moves_out())
-        for_eights<THREADS>(0, a.keep, [&](const int (&j)[8]) {
+        for_some<THREADS, N>(0, a.keep, [&](const int (&j)[N]) {
             if constexpr (!SHORT) load(j);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < N; ++e) {
                 const uint32_t stays = SHORT ? rank[e] : ranks[min(j[e], n - 1)];
                 if (j[e] < a.keep && stays) r.leave(j[e], x[e], o[e]);
             }
         });
+    if (a.at_once) do_moves<THREADS>(a, row, n_moves);   // (behind a barrier: the list is there)
+    else if (tid == 0) a.counts[row] = n_moves;
+}
+
+// The lengths, for a call whose first kernel also moves: its workgroups read them.
+__global__ __launch_bounds__(kMoveThreads) void evict_lengths(const EvictArgs a)
+{
+    const int seq = blockIdx.x * kMoveThreads + threadIdx.x;
+    if (seq < a.cache.n_seqs) a.lens_out[seq] = min(used_slots(a, seq), a.keep);
 }
 
 // ------------------------------------------------------------------------------------ rows in chunks
@@ -381,7 +433,7 @@ __global__ __launch_bounds__(kChunkThreads) void evict_newest(const EvictArgs a)
         return;
     }
     int newest = INT32_MIN;
-    for_eights<kChunkThreads>(c.begin, c.end, [&](const int (&j)[8]) {
+    for_some<kChunkThreads, 8>(c.begin, c.end, [&](const int (&j)[8]) {
         int32_t o[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = r.order[min(j[e], c.end - 1)];
@@ -435,7 +487,7 @@ struct Eight {
 template <typename F>
 __device__ inline void for_ranks(const EvictArgs &a, const Row &r, const Chunk &c, Eight &v, int32_t newest, F f)
 {
-    for_eights<kChunkThreads>(c.begin, c.end, [&](const int (&j)[8]) {
+    for_some<kChunkThreads, 8>(c.begin, c.end, [&](const int (&j)[8]) {
         if (j[0] != c.begin + (int)threadIdx.x) v.load(r, c, j);
         uint32_t rank[8];
 #pragma unroll
@@ -558,67 +610,36 @@ __global__ __launch_bounds__(kChunkThreads) void evict_list(const EvictArgs a)
         __syncthreads();
         for (int i = tid >> 6; i < kChunkThreads && (w0 + i) * 64 < c.end; i += kChunkThreads / 64) {
             const uint64_t x = lists[i];
-            if ((x >> lane) & 1) moves[places[i] + __popcll(x & ((1ull << lane) - 1))] = (w0 + i) * 64 + lane;
+            const int at = places[i] + __popcll(x & ((1ull << lane) - 1));   // holes first
+            if ((x >> lane) & 1) moves[at < all_listed / 2 ? at : 2 * a.max_moves - all_listed + at] = (w0 + i) * 64 + lane;
         }
         __syncthreads();
     }
 }
 
-__device__ inline int64_t slot_offset(const bs_cache &c, int seq, int head, int slot)   // -1: no page
-{
-    const int page = c.page_table[(int64_t)seq * c.max_pages + slot / c.page_size];
-    if (page < 0 || page >= c.n_pages) return -1;
-    return page * c.page_stride + head * c.head_stride + (slot % c.page_size) * c.slot_stride;
-}
-
-// `count` moves, each by as many threads as a row has pieces of 16 bytes.
-template <typename T, typename M>
-__device__ inline void do_moves(const EvictArgs &a, int row, int count, M move)
-{
-    const int seq = row / a.cache.n_kv_heads, head = row - seq * a.cache.n_kv_heads;
-    constexpr int PER = 16 / sizeof(T);
-    const unsigned pieces = a.cache.head_dim / PER;
-    const T *k = static_cast<const T *>(a.cache.k), *v = static_cast<const T *>(a.cache.v);
-    for (unsigned idx = threadIdx.x; idx < count * pieces; idx += kMoveThreads) {
-        const unsigned i = idx / pieces, p = idx - i * pieces;
-        const int2 m = move(i);   // to, from
-        const int64_t dst = slot_offset(a.cache, seq, head, m.x), src = slot_offset(a.cache, seq, head, m.y);
-        if (dst >= 0 && src >= 0) {
-            const uint4 x = *reinterpret_cast<const uint4 *>(k + src + p * PER), y = *reinterpret_cast<const uint4 *>(v + src + p * PER);
-            *reinterpret_cast<uint4 *>(const_cast<T *>(k) + dst + p * PER) = x;
-            *reinterpret_cast<uint4 *>(const_cast<T *>(v) + dst + p * PER) = y;
-        }
-        if (p == 0) {
-            a.weights_out[row * a.out_stride + m.x] = a.weights[row * a.in_stride + m.y];
-            a.order_out[row * a.out_stride + m.x] = a.order[row * a.in_stride + m.y];
-        }
-    }
-}
-
-// (the kernels before have read the lengths)
-__device__ inline void set_length(const EvictArgs &a, int row)
-{
-    if (blockIdx.y == 0 && row % a.cache.n_kv_heads == 0 && threadIdx.x == 0) {
-        const int seq = row / a.cache.n_kv_heads;
-        a.lens_out[seq] = min(used_slots(a, seq), a.keep);
-    }
-}
-
-// Moves [first, first + count) of this workgroup.
-__device__ inline int2 own_moves(int n)
-{
-    const int each = (n + (int)gridDim.y - 1) / (int)gridDim.y, first = min(n, (int)blockIdx.y * each);
-    return make_int2(first, min(each, n - first));
-}
-
-template <typename T>
+// A move by as many threads as a row has pieces of 16 bytes.
 __global__ __launch_bounds__(kMoveThreads) void evict_move(const EvictArgs a)
 {
-    const int row = blockIdx.x, n = a.counts[row];
+    const int row = blockIdx.x, n = a.counts[row], seq = row / a.cache.n_kv_heads, head = row - seq * a.cache.n_kv_heads;
+    const int bytes = a.cache.dtype == BS_BF16 ? 2 : 4, pieces = a.cache.head_dim * bytes / 16;
     const int32_t *moves = a.moves + (int64_t)row * 2 * a.max_moves;
-    const int2 own = own_moves(n);
-    do_moves<T>(a, row, own.y, [&](int i) { return make_int2(moves[own.x + i], moves[n + own.x + i]); });
-    set_length(a, row);
+    char *k = static_cast<char *>(a.cache.k), *v = static_cast<char *>(a.cache.v);
+    for (int64_t idx = (int64_t)blockIdx.y * kMoveThreads + threadIdx.x; idx < (int64_t)n * pieces; idx += (int64_t)gridDim.y * kMoveThreads) {
+        const int i = (int)(idx / pieces), p = (int)(idx - (int64_t)i * pieces);
+        const int to = moves[i], from = moves[2 * a.max_moves - n + i];
+        const int64_t dst = slot_offset(a.cache, seq, head, to), src = slot_offset(a.cache, seq, head, from);
+        if (dst >= 0 && src >= 0) {
+            const uintx4 x = *reinterpret_cast<const uintx4 *>(k + src * bytes + 16 * p), y = *reinterpret_cast<const uintx4 *>(v + src * bytes + 16 * p);
+            *reinterpret_cast<uintx4 *>(k + dst * bytes + 16 * p) = x;
+            *reinterpret_cast<uintx4 *>(v + dst * bytes + 16 * p) = y;
+        }
+        if (p == 0) {
+            a.weights_out[row * a.out_stride + to] = a.weights[row * a.in_stride + from];
+            a.order_out[row * a.out_stride + to] = a.order[row * a.in_stride + from];
+        }
+    }
+    // (the kernels before have read the lengths)
+    if (blockIdx.y == 0 && head == 0 && threadIdx.x == 0) a.lens_out[seq] = min(used_slots(a, seq), a.keep);
 }
 
 int check_evict(const bs_cache *cache, int32_t keep)
@@ -632,6 +653,7 @@ int check_evict(const bs_cache *cache, int32_t keep)
 struct Plan {
     int64_t rows, moves;
     int32_t chunks, words;      // chunks 0: one workgroup per row
+    bool at_once;
     int64_t at_moves, at_need, at_newest, at_hist, at_above, at_ties, at_marked, bytes;
 };
 
@@ -641,10 +663,13 @@ Plan make_plan(const bs_cache &c, int32_t keep)
     const int64_t capacity = cache_slots(c);
     p.rows = (int64_t)c.n_seqs * c.n_kv_heads;
     p.moves = std::max<int64_t>(0, std::min<int64_t>(keep, capacity - keep));
-    if (capacity > kRanksMax || (p.rows <= 32 && capacity > 4096)) {
+    // Rows beyond what LDS holds, and few long ones, whose CUs would be too few.  Cut back to half, a workgroup each / in chunks: 4 rows of 8K slots
+    // 17.9 / 32.1 us, of 16K 30.3 / 33.6, of 30K 50.9 / 37.1; 32 rows 32.5 / 48.0, 59.7 / 65.2, 102 / 94.
+    if (capacity > kRanksMax || (p.rows <= 32 && capacity > 20480)) {
         p.chunks = (int32_t)std::max<int64_t>(1, std::min<int64_t>({64, (capacity + 1023) / 1024, (1024 + p.rows - 1) / p.rows}));
         p.words = (int32_t)((capacity + 63) / 64);
     }
+    p.at_once = p.chunks == 0 && p.moves <= kMovesAtOnce;   // (512 rows of 4160 slots, 64 moves: 34.2 us with a kernel for the moves, 31.0 so)
     const auto whole = [](int64_t bytes) { return (bytes + 255) / 256 * 256; };
     p.at_moves = whole(p.rows * 4);
     p.at_need = p.at_moves + whole(p.rows * p.moves * 8);
@@ -668,7 +693,7 @@ hipError_t device_setup()
     if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
     std::lock_guard<std::mutex> lock(g_mutex);
     if (g_limits[dev]) return hipSuccess;
-    const void *const k = reinterpret_cast<const void *>(evict_select<1024, false>);
+    const void *const k = reinterpret_cast<const void *>(evict_select<1024, 0>);
     if ((e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kRanksMax * 4)) != hipSuccess) return e;
     g_limits[dev] = true;
     return hipSuccess;
@@ -679,12 +704,14 @@ hipError_t launch_select(const EvictArgs &a, const Plan &p, hipStream_t st)
     const int64_t capacity = cache_slots(a.cache);
     if (p.chunks == 0) {
         const dim3 grid((unsigned)p.rows);
-        // as few threads as have eight slots each: their barriers are cheaper, and more rows fit a CU
-        if (capacity <= 8 * 256) return launch_kernel(evict_select<256, true>, grid, dim3(256), 0, st, a);
-        if (capacity <= 8 * 512) return launch_kernel(evict_select<512, true>, grid, dim3(512), 0, st, a);
-        if (capacity <= 8 * 1024) return launch_kernel(evict_select<1024, true>, grid, dim3(1024), 0, st, a);
+        // Eight slots a thread; more only where there are more rows than CUs, which then share one: what a wave does besides its slots (scans,
+        // barriers) counts.  Rows of 4160 slots, with 1024 threads / 512 of 16 slots: 512 rows 39.9 / 31.0 us, 128 of 8000 22.8 / 28.1.
+        if (capacity <= 8 * 256) return launch_kernel(evict_select<256, 8>, grid, dim3(256), 0, st, a);
+        if (capacity <= 8 * 512) return launch_kernel(evict_select<512, 8>, grid, dim3(512), 0, st, a);
+        if (capacity <= 8 * 1024 && p.rows <= 256) return launch_kernel(evict_select<1024, 8>, grid, dim3(1024), 0, st, a);
+        if (capacity <= 16 * 512) return launch_kernel(evict_select<512, 16>, grid, dim3(512), 0, st, a);
         if (const hipError_t e = device_setup(); e != hipSuccess) return e;
-        return launch_kernel(evict_select<1024, false>, grid, dim3(1024), (capacity + 1023) / 1024 * 4096, st, a);
+        return launch_kernel(evict_select<1024, 0>, grid, dim3(1024), (capacity + 1023) / 1024 * 4096, st, a);
     }
     const dim3 grid((unsigned)p.rows, (unsigned)p.chunks), block(kChunkThreads);
     hipError_t e = launch_kernel(evict_newest, grid, block, 0, st, a);
@@ -727,6 +754,7 @@ extern "C" int bs_cache_evict(const bs_cache *cache, const int32_t *lens, int32_
     a.counts = reinterpret_cast<int32_t *>(ws);
     a.moves = reinterpret_cast<int32_t *>(ws + p.at_moves);
     a.max_moves = (int32_t)p.moves;
+    a.at_once = p.at_once;
     a.chunks = p.chunks;
     a.need = reinterpret_cast<int32_t *>(ws + p.at_need);
     a.newest = reinterpret_cast<int32_t *>(ws + p.at_newest);
@@ -738,10 +766,13 @@ extern "C" int bs_cache_evict(const bs_cache *cache, const int32_t *lens, int32_
     hipStream_t st = (hipStream_t)stream;
     hipError_t e = launch_select(a, p, st);
     if (e != hipSuccess) return fail_hip(e, "eviction: select launch");
+    const dim3 block(kMoveThreads);
+    if (p.at_once) {
+        e = launch_kernel(evict_lengths, dim3((unsigned)((cache->n_seqs + kMoveThreads - 1) / kMoveThreads)), block, 0, st, a);
+        return e == hipSuccess ? BS_OK : fail_hip(e, "evict_lengths launch");
+    }
     const int64_t pieces = (int64_t)cache->head_dim * element_bytes(cache->dtype) / 16;
     const int64_t blocks = std::max<int64_t>(1, std::min({(p.moves * pieces + kMoveThreads - 1) / kMoveThreads, (int64_t)1024, (4096 + p.rows - 1) / p.rows}));
-    const dim3 grid((unsigned)p.rows, (unsigned)blocks);
-    const dim3 block(kMoveThreads);
-    e = cache->dtype == BS_BF16 ? launch_kernel(evict_move<__bf16>, grid, block, 0, st, a) : launch_kernel(evict_move<float>, grid, block, 0, st, a);
+    e = launch_kernel(evict_move, dim3((unsigned)p.rows, (unsigned)blocks), block, 0, st, a);
     return e == hipSuccess ? BS_OK : fail_hip(e, "evict_move launch");
 }

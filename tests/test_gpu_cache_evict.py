@@ -69,11 +69,11 @@ def test_evict(dtype, hkv, d, page, pool, keep, first, last, in_place):
     run(c, keep, first, last, *draw(c, keep), in_place)
 
 
-@pytest.mark.parametrize("lens", [[6000, 0, 63], [1, 8193, 200, 20000, 5, 777] * 9, [5000, 3, 7000] * 14, [3000, 4000] * 20])
+@pytest.mark.parametrize("lens", [[23000, 0, 63, 6000], [1, 8193, 200, 20000, 5, 777] * 9, [5000, 3, 7000] * 14, [5000, 3, 7000] * 90, [3000, 4000] * 20])
 @pytest.mark.parametrize("keep,first,last", [(1, 0, 1), (200, 4, 196), (1023, 5, 100), (5000, 0, 0)])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_rows_of_other_lengths(lens, keep, first, last, in_place):
-    """In chunks; one workgroup each with ranks in LDS; one each with ranks in registers, of 1024 and of 512 threads."""
+    """In chunks; one workgroup each with ranks in LDS; one each with ranks in registers, of 1024 threads, of 512 with 16 and with 8 slots."""
     c = Paged("bf16", 1, 8, 16, lens, seed=keep)
     run(c, keep, first, last, *draw(c, keep), in_place)
 
@@ -85,7 +85,7 @@ def test_long(n, keep):
 
 
 @pytest.mark.parametrize("values", ["equal", "zeros", "few", "special", "one bit apart"])
-@pytest.mark.parametrize("capacity", [3008, 6000, 40000])   # few rows: one workgroup each, or in chunks
+@pytest.mark.parametrize("capacity", [3008, 6000, 18000, 40000])   # few rows: one workgroup each, ranks in LDS, or in chunks
 def test_ties_and_special_weights(values, capacity):
     make = lambda: Paged("bf16", 2, 8, 16, [700, 3000], capacity=capacity, seed=2)
     c = make()
@@ -106,7 +106,7 @@ def test_ties_and_special_weights(values, capacity):
         run(make(), keep, 0, 0, w, order, False)
 
 
-@pytest.mark.parametrize("capacity", [1008, 5000])
+@pytest.mark.parametrize("capacity", [1008, 5000, 16000, 24000])
 def test_orders_that_an_eviction_mixed(capacity):
     c = Paged("bf16", 2, 64, 16, [500, 900], capacity=capacity, seed=3)
     w, order = draw(c, 7)

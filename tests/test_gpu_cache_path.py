@@ -161,7 +161,7 @@ def fill(layer, lens, gen):
     torch.cuda.synchronize()
 
 
-@pytest.mark.parametrize("capacity,keep,lens", [(512, 300, [300, 7, 0, 299]), (6000, 4500, [4500, 0, 4499]), (40960, 3000, [2999] * 40)])
+@pytest.mark.parametrize("capacity,keep,lens", [(512, 300, [300, 7, 0, 299]), (6000, 4500, [4500, 0, 4499]), (24576, 300, [299, 300, 4]), (40960, 3000, [2999] * 40)])
 def test_replays_of_a_captured_step(capacity, keep, lens):
     """Append, decode and evict in one graph, replayed, with eager work between the replays, against the same steps run eagerly."""
     make = lambda: Layer(len(lens), 8, 2, 64, 16, capacity, seed=3)
