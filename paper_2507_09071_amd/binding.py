@@ -461,6 +461,8 @@ class KVCache(ctypes.Structure):
         page_table: contiguous int32 [n_seqs, max_pages]."""
         if k.shape != v.shape or k.stride() != v.stride() or k.stride()[3] != 1:
             raise ValueError("k and v have to be alike in shape and strides, with contiguous channels")
+        if k.element_size() != (2 if dtype == BS_BF16 else 4):
+            raise ValueError("dtype does not fit the pools")
         n_seqs, max_pages = page_table.shape
         if not page_table.is_contiguous() or page_table.element_size() != 4:
             raise ValueError("page_table has to be contiguous int32")

@@ -104,8 +104,7 @@ __device__ inline void rotation(double quarter_turns, int32_t position, float &c
 template <typename T, int V, bool HALF>
 __global__ __launch_bounds__(kThreads) void rope_rows(const RopeArgs a)
 {
-    const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int64_t per_split = (int64_t)a.n_tokens * a.groups;
+    const uint32_t idx = blockIdx.x * kThreads + threadIdx.x, per_split = a.n_tokens * a.groups;
     const int split = (int)(idx / per_split);
     if (split >= a.head_splits) return;
     const int item = (int)(idx - split * per_split);
@@ -225,11 +224,10 @@ int run_rope(RopeArgs &a, const bs_rope *rope, int32_t dtype, int32_t head_dim, 
     for (int j = 0; j < a.n_jobs; ++j) a.n_heads += a.jobs[j].n_heads;
     // Heads share a thread's angles; where there are too few tokens to fill the chip they are split over threads.
     const int64_t items = (int64_t)a.n_tokens * a.groups;
-    if (items > INT32_MAX) return BS_EUNSUPPORTED;
+    if (items > INT32_MAX) return BS_EUNSUPPORTED;   // (with several splits there are few, so threads are counted in 32 bits)
     a.head_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(a.n_heads, (256 * 2048 + items - 1) / items));
     a.heads_each = (a.n_heads + a.head_splits - 1) / a.head_splits;
     a.head_splits = (a.n_heads + a.heads_each - 1) / a.heads_each;
-    if ((items * a.head_splits + kThreads - 1) / kThreads > INT32_MAX) return BS_EUNSUPPORTED;
     const bool half = !rope || rope->layout == BS_ROPE_HALF;
     hipError_t err;
     if (dtype == BS_BF16) err = half ? launch_layout<__bf16, true>(a, vec, st) : launch_layout<__bf16, false>(a, vec, st);

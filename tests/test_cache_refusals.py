@@ -153,6 +153,8 @@ def test_views_that_the_binding_refuses():
     with pytest.raises(ValueError):
         bs.KVCache.of(k, k, torch.zeros((1, 2), dtype=torch.int64), bs.BS_F32)
     with pytest.raises(ValueError):
+        bs.KVCache.of(k, k, torch.zeros((1, 2), dtype=torch.int32), bs.BS_BF16)
+    with pytest.raises(ValueError):
         bs.CacheSlots.of()
     with pytest.raises(ValueError):
         bs.CacheSlots.of(torch.zeros(1, 2, 5), torch.zeros((1, 2, 6), dtype=torch.int32))

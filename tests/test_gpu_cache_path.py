@@ -67,7 +67,8 @@ def expect(layer, s, q, keys, values):
     n = keys.shape[1]
     S = float((q.abs().view(layer.hkv, g, -1) @ keys.abs().transpose(1, 2)).max() * layer.d ** -0.5)
     step = (2 * layer.d * S + n + 64) * 2.0 ** -24
-    tol = 2 * step * spread + (2.0 ** -8 * 1.01 * (spread + out.abs()) if layer.dtype == "bf16" else 2.0 ** -24 * out.abs())
+    tol = 2 * step * spread + (2.0 ** -16 * spread if layer.dtype == "bf16" else 0)
+    tol = tol + (2.0 ** -8 if layer.dtype == "bf16" else 2.0 ** -24) * (out.abs() + tol)
     return out.flatten(0, 1), tol.flatten(0, 1), p.sum(1), 2 * step * p.sum(1) + (g + 2) * 2.0 ** -24 * p.sum(1)
 
 
