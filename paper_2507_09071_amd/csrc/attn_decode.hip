@@ -1,7 +1,12 @@
 // Attention of one new token per sequence over a paged cache.
 //
 // What has to be done is reading K and V of every visible slot once, so the bound is HBM: 4 d FLOP for every query head of a group
-// and slot are at most a few dozen per byte, which the matrix pipe does on the side.  How:
+// and slot are at most a few dozen per byte, which the matrix pipe does on the side (busy 6 % of the time).  Measured: two sequences of 150K
+// slots, 32 / 16 heads of 128, 2.46 GB: 412 us, 6.0 TB/s, what a kernel that only reads reaches; one of 39.5K, 28 / 4 heads, 81 MB: 23.4 us, of
+// which the two kernels are 17.4 and 4.0 (13 at that rate); 48 sequences of 17 to 16K slots, 40 / 8 heads, 498 MB: 102 us; fp32, 32 / 8 heads, four
+// sequences of 8K to 16K: 77 us, 5.0 TB/s.  Tried: half as many waves in twice as many workgroups (412 -> 448), a wave per short item (256 sequences of
+// 5 to 300 slots, two heads a group: 70 -> 56, but 200 of 200 to 2K 70 -> 72 and more), query rows and page numbers of the next item ahead of
+// time (nothing).  How:
 //  * the query heads of a KV head are the free dimension of a 16x16 MFMA (one block of 16 rows, or two; groups of 32 beyond that), so K and
 //    V are read once for all of them;
 //  * the work of all sequences and KV heads ("items") is one row of blocks of 32 slots (16 in fp32: the same bytes), cut into equal
@@ -220,7 +225,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void decode_shares(const
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(newer)::value) : "memory");
     };
     const auto reads_done = []() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
-    // Stores of scores count among the loads in flight.  Those of the second row block are not counted: there may be none.
+    // Stores of scores count among the loads in flight.  Those of the second row block are not counted: there may be none.  (What they cost, 412 -> 475
+    // us for two sequences of 150K slots with two heads a group, is the same with half as many, with four blocks' together, past the caches, and to a
+    // few lines over and over: memory turns around for them.)
     constexpr int NS = WEIGHTS ? SUB : 0;
 
     const uint32_t k_read = wave * TR::kWave + col * ROWB + ((grp ^ TR::swizzle(col)) << 4);

@@ -1,7 +1,9 @@
 // Rotary positions, and new tokens into a paged cache (which rotates on the way).
 //
 // A pair (a, b) of channels is turned by the angle position * f: (a cos - b sin, b cos + a sin).  The work is reading every row once
-// and writing it once, so the bound is HBM, and what an angle costs has to be paid once per token and pair, not once per head.
+// and writing it once, so the bound is HBM, and what an angle costs has to be paid once per token and pair, not once per head: a thread keeps its
+// angles over the heads.  39.5K tokens of 28 + 4 heads, 648 MB: 124 us, 5.2 TB/s, a large copy's rate (5.0 to 5.5); the same into pages, token-major
+// rows, 730 MB: 154 us, 4.75 TB/s.  (Stores past the caches: 121 and 151 us, but 50 -> 67 for rows of which an instruction writes half a line.)
 #include <algorithm>
 #include <cmath>
 #include <cstring>
