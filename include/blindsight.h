@@ -422,7 +422,8 @@ double bs_alpha_layer(double alpha_first, double alpha_last, int32_t layer_idx, 
  * overlap, and graphs that may be replayed at the same time, need one each.  All pointers are device pointers of the
  * current HIP device unless they say host, and `stream` is one of its streams.  Threads may call at the same time.
  * Errors of all of them: BS_EINVAL (null pointers, sizes or strides that cannot be, a workspace that is too small),
- * BS_EUNSUPPORTED (dtype, head_dim, page size or alignment that the kernels do not implement), BS_EHIP.  Nothing is launched on error.
+ * BS_EUNSUPPORTED (dtype, head_dim, page size, alignment or a size beyond 32 bits that the kernels do not implement), BS_EHIP.  Nothing is
+ * launched on error.
  */
 
 /* Some heads of some tokens: element c of head h of token t at data[h * head_stride + t * token_stride + c], strides in
@@ -467,7 +468,7 @@ int bs_rope_init(bs_rope *rope, int32_t rotary_dim, int32_t layout, double base,
 /*
  * Apply rotary positions to n_tensors (1 or 2: q and k of a layer) sets of heads of the same tokens.
  *   x, y       host, [n_tensors]; y[i] as many heads as x[i].  y may be x itself (same data and strides), else they do
- *              not overlap
+ *              not overlap; rows of y lie apart (BS_EINVAL), those of x may be the same one (stride 0)
  *   head_dim   even, rotary_dim <= head_dim <= 2 * BS_ROPE_MAX_PAIRS
  *   positions  device, row a = axis a, axis_stride elements apart: positions[a * axis_stride + t], any 32-bit value
  *   flags      0 or BS_ROPE_INVERSE
@@ -479,7 +480,7 @@ int bs_rope_apply(const bs_rope *rope, const bs_heads *x, const bs_heads *y, int
 
 /* A KV cache in pages.  Slot j of sequence s and KV head h lies in page p = page_table[s * max_pages + j / page_size] at
  * k[p * page_stride + h * head_stride + (j % page_size) * slot_stride], head_dim contiguous elements, and likewise in v; strides in
- * elements, so that [page][head][slot][d] and [page][slot][head][d] both fit.  A page number outside [0, n_pages) means that these
+ * elements and at least head_dim where the cache is written, so that [page][head][slot][d] and [page][slot][head][d] both fit.  A page number outside [0, n_pages) means that these
  * slots have no page: they are not written, and nobody sees them.  k and v 16-byte aligned, strides multiples of 16 bytes;
  * head_dim a multiple of 8 up to 256 (bs_attn_decode: 64 or 128), page_size a multiple of 16. */
 typedef struct {

@@ -509,8 +509,9 @@ def bs_rope_apply(rope: Rope, xs, ys, dtype: int, n_tokens: int, head_dim: int, 
     n = len(xs)
     if len(ys) != n:
         raise ValueError("as many ys as xs")
-    rc = load_library().bs_rope_apply(ctypes.byref(rope), b"".join(map(_heads, xs)), b"".join(map(_heads, ys)), n, dtype, n_tokens, head_dim,
-                                      _ptr(positions), n_tokens if axis_stride is None else axis_stride, BS_ROPE_INVERSE if inverse else 0, stream or None)
+    rc = load_library().bs_rope_apply(ctypes.byref(rope), b"".join(map(_heads, xs)), b"".join(map(_heads, ys)), n, int(dtype), int(n_tokens),
+                                      int(head_dim), _ptr(positions), int(n_tokens if axis_stride is None else axis_stride),
+                                      BS_ROPE_INVERSE if inverse else 0, int(stream) if stream else None)
     _check(rc, "bs_rope_apply")
 
 
@@ -518,9 +519,9 @@ def bs_cache_append(cache: KVCache, k, v, n_tokens: int, token_seq, token_slot, 
                     axis_stride: int | None = None, q=None, q_out=None, slots: CacheSlots | None = None, token_order=None, stream=None) -> None:
     """k, v, q, q_out: tensors [n_heads, n_tokens, head_dim] of any strides (or Heads); token_seq (None: token t is of sequence t),
     token_slot, token_order (None: the slot's number): int32 on the device.  Enqueues only."""
-    rc = load_library().bs_cache_append(ctypes.byref(cache), _heads(k), _heads(v), n_tokens, _address(token_seq), _ptr(token_slot), _ref(rope),
-                                        _address(positions), n_tokens if axis_stride is None else axis_stride, None if q is None else _heads(q),
-                                        None if q_out is None else _heads(q_out), _ref(slots), _address(token_order), stream or None)
+    rc = load_library().bs_cache_append(ctypes.byref(cache), _heads(k), _heads(v), int(n_tokens), _address(token_seq), _ptr(token_slot), _ref(rope),
+                                        _address(positions), int(n_tokens if axis_stride is None else axis_stride), None if q is None else _heads(q),
+                                        None if q_out is None else _heads(q_out), _ref(slots), _address(token_order), int(stream) if stream else None)
     _check(rc, "bs_cache_append")
 
 
@@ -536,8 +537,8 @@ def bs_attn_decode(cache: KVCache, q, out, lens, scale: float, workspace, window
                    slots_out: CacheSlots | None = None, stream=None) -> None:
     """q, out: tensors [n_q_heads, n_seqs, head_dim] of any strides (or Heads); lens: int32 [n_seqs] on the device; workspace: a tensor, or
     (address, bytes), of bs_attn_decode_workspace bytes.  slots, slots_out: add up the attention that every slot receives.  Enqueues only."""
-    rc = load_library().bs_attn_decode(ctypes.byref(cache), _heads(q), _heads(out), _ptr(lens), window, scale, _ref(slots), _ref(slots_out),
-                                       *_buffer(workspace), stream or None)
+    rc = load_library().bs_attn_decode(ctypes.byref(cache), _heads(q), _heads(out), _ptr(lens), int(window), float(scale), _ref(slots),
+                                       _ref(slots_out), *_buffer(workspace), int(stream) if stream else None)
     _check(rc, "bs_attn_decode")
 
 
@@ -552,8 +553,8 @@ def bs_cache_evict(cache: KVCache, lens, lens_out, keep: int, keep_first: int, k
                    stream=None) -> None:
     """lens, lens_out: int32 [n_seqs] on the device, may be the same, as slots and slots_out; workspace: a tensor, or (address, bytes), of
     bs_cache_evict_workspace bytes.  Enqueues only."""
-    rc = load_library().bs_cache_evict(ctypes.byref(cache), _ptr(lens), _ptr(lens_out), keep, keep_first, keep_last, _ref(slots), _ref(slots_out),
-                                       *_buffer(workspace), stream or None)
+    rc = load_library().bs_cache_evict(ctypes.byref(cache), _ptr(lens), _ptr(lens_out), int(keep), int(keep_first), int(keep_last), _ref(slots),
+                                       _ref(slots_out), *_buffer(workspace), int(stream) if stream else None)
     _check(rc, "bs_cache_evict")
 
 

@@ -800,6 +800,7 @@ extern "C" int bs_attn_decode(const bs_cache *cache, const bs_heads *q, const bs
         if (window > 0) return BS_EUNSUPPORTED;
     }
     if (!rows_aligned(*q, cache->dtype) || !rows_aligned(*out, cache->dtype)) return BS_EUNSUPPORTED;
+    if (int rc = check_rows_apart(*out, cache->n_seqs, cache->head_dim)) return rc;
     if (q->head_stride * element_bytes(cache->dtype) * 32 > INT32_MAX) return BS_EUNSUPPORTED;   // rows of a group are addressed in 32 bits
     int n_cus = 0;
     Plan p;

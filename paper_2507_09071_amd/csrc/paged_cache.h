@@ -16,6 +16,9 @@ constexpr int64_t kMaxStride = (int64_t)1 << 40;
 
 int check_cache(const bs_cache *c);
 int check_heads(const bs_heads *h);   // data, sizes and strides
+// Rows that are written lie apart from each other.
+int check_rows_apart(const bs_heads &h, int32_t n_tokens, int32_t head_dim);
+int check_rows_apart(const bs_cache &c);
 // Rows of the cache's sequences and KV heads; `row_stride` has to hold their slots.
 int check_slots(const bs_cache &c, const bs_slots *s);
 // 16-byte loads of whole rows: pointer and strides allow them.

@@ -36,6 +36,19 @@ int check_heads(const bs_heads *h)
     return BS_OK;
 }
 
+int check_rows_apart(const bs_heads &h, int32_t n_tokens, int32_t head_dim)
+{
+    const bool heads = h.n_heads > 1, tokens = n_tokens > 1;
+    if ((heads && h.head_stride < head_dim) || (tokens && h.token_stride < head_dim)) return BS_EINVAL;
+    if (heads && tokens && h.head_stride < h.token_stride * (n_tokens - 1) + head_dim && h.token_stride < h.head_stride * (h.n_heads - 1) + head_dim) return BS_EINVAL;
+    return BS_OK;
+}
+
+int check_rows_apart(const bs_cache &c)
+{
+    return (c.n_kv_heads > 1 && c.head_stride < c.head_dim) || c.slot_stride < c.head_dim || (c.n_pages > 1 && c.page_stride < c.head_dim) ? BS_EINVAL : BS_OK;
+}
+
 int check_slots(const bs_cache &c, const bs_slots *s)
 {
     return s->row_stride < cache_slots(c) || s->row_stride > kMaxStride || ((uintptr_t)s->weights | (uintptr_t)s->order) % 4 != 0 ? BS_EINVAL : BS_OK;
@@ -309,7 +322,7 @@ extern "C" int bs_rope_apply(const bs_rope *rope, const bs_heads *x, const bs_he
     a.n_jobs = n_tensors;
     for (int i = 0; i < n_tensors; ++i) {
         if (check_heads(&x[i]) || check_heads(&y[i]) || x[i].n_heads != y[i].n_heads || x[i].n_heads > (1 << 20)) return BS_EINVAL;
-        if (((uintptr_t)x[i].data | (uintptr_t)y[i].data) % element_bytes(dtype) != 0) return BS_EINVAL;
+        if (((uintptr_t)x[i].data | (uintptr_t)y[i].data) % element_bytes(dtype) != 0 || check_rows_apart(y[i], n_tokens, head_dim)) return BS_EINVAL;
         a.jobs[i] = job_of(x[i], y[i], true);
     }
     a.n_tokens = n_tokens;
@@ -326,7 +339,8 @@ extern "C" int bs_cache_append(const bs_cache *cache, const bs_heads *k, const b
     if (int rc = check_cache(cache)) return rc;
     if (check_heads(k) || check_heads(v) || !token_slot || n_tokens < 0) return BS_EINVAL;
     if (k->n_heads != cache->n_kv_heads || v->n_heads != cache->n_kv_heads || !q != !q_out || (q && !rope)) return BS_EINVAL;
-    if (q && (check_heads(q) || check_heads(q_out) || q->n_heads != q_out->n_heads || q->n_heads > (1 << 20))) return BS_EINVAL;
+    if (q && (check_heads(q) || check_heads(q_out) || q->n_heads != q_out->n_heads || q->n_heads > (1 << 20) || check_rows_apart(*q_out, n_tokens, cache->head_dim))) return BS_EINVAL;
+    if (int rc = check_rows_apart(*cache)) return rc;
     if (rope)
         if (int rc = check_rope(rope, cache->head_dim, positions, axis_stride)) return rc;
     if (slots)

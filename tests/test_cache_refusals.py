@@ -45,6 +45,14 @@ def test_caches(bad, code):
     assert lib.bs_attn_decode_workspace(ref(c), 8, 0) == code
 
 
+@pytest.mark.parametrize("bad", [dict(head_stride=0), dict(slot_stride=120), dict(slot_stride=0), dict(page_stride=64)])
+def test_caches_whose_rows_overlap_are_not_written(bad):
+    lib, c, h, s = binding.load_library(), cache(**bad), heads(4), bs.CacheSlots(P, P, 112)
+    assert lib.bs_cache_append(ref(c), ref(h), ref(h), 3, None, P, None, None, 0, None, None, None, None, None) == EINVAL
+    assert lib.bs_cache_evict(ref(c), P, P, 5, 0, 0, ref(s), ref(s), P, 1 << 40, None) == EINVAL
+    assert lib.bs_cache_evict_workspace(ref(c), 5) == EINVAL
+
+
 def test_no_cache():
     lib, h = binding.load_library(), heads(4)
     assert lib.bs_cache_append(None, ref(h), ref(h), 3, None, P, None, None, 0, None, None, None, None, None) == EINVAL
@@ -57,7 +65,7 @@ def test_no_cache():
     (dict(scale=math.inf), EINVAL), (dict(scale=-1.0), EINVAL), (dict(slots=None), EINVAL), (dict(slots_out=None), EINVAL), (dict(workspace=None), EINVAL),
     (dict(workspace=P + 8), EINVAL), (dict(n_bytes=-1), EINVAL), (dict(slots=bs.CacheSlots(None, P, 112)), EINVAL), (dict(slots=bs.CacheSlots(P, P, 111)), EINVAL),
     (dict(slots=bs.CacheSlots(P, P, 120)), EINVAL), (dict(slots_out=bs.CacheSlots(P + 2, P, 112)), EINVAL), (dict(window=5), EUNSUPPORTED),
-    (dict(q=heads(data=P + 8)), EUNSUPPORTED), (dict(out=heads(head=132)), EUNSUPPORTED), (dict(q=heads(token=-8)), EINVAL), (dict(cache=cache(head_dim=256)), EUNSUPPORTED),
+    (dict(q=heads(data=P + 8)), EUNSUPPORTED), (dict(out=heads(head=132)), EUNSUPPORTED), (dict(out=heads(head=0)), EINVAL), (dict(out=heads(token=512)), EINVAL), (dict(q=heads(token=-8)), EINVAL), (dict(cache=cache(head_dim=256)), EUNSUPPORTED),
     (dict(cache=cache(head_dim=96)), EUNSUPPORTED)])
 def test_decode(change, code):
     f = dict(cache=cache(), q=heads(), out=heads(), lens=P, window=0, scale=0.1, slots=bs.CacheSlots(P, P, 112), slots_out=bs.CacheSlots(P, P, 112), workspace=P, n_bytes=1 << 40)
@@ -105,7 +113,7 @@ def broken(**kw):
 @pytest.mark.parametrize("change,code", [
     (dict(rope=None), EINVAL), (dict(x=None), EINVAL), (dict(n_tensors=0), EINVAL), (dict(n_tensors=3), EINVAL), (dict(dtype=2), EUNSUPPORTED), (dict(n=-1), EINVAL),
     (dict(d=62), EINVAL), (dict(d=129), EINVAL), (dict(d=258), EINVAL), (dict(positions=None), EINVAL), (dict(axis_stride=-1), EINVAL), (dict(flags=2), EINVAL),
-    (dict(y=heads(7)), EINVAL), (dict(x=heads(data=P + 1)), EINVAL), (dict(x=heads(token=-1)), EINVAL), (dict(rope=broken(rotary_dim=63)), EINVAL),
+    (dict(y=heads(head=64)), EINVAL), (dict(y=heads(token=0)), EINVAL), (dict(y=heads(token=1016)), EINVAL), (dict(y=heads(head=300, token=128)), EINVAL), (dict(y=heads(7)), EINVAL), (dict(x=heads(data=P + 1)), EINVAL), (dict(x=heads(token=-1)), EINVAL), (dict(rope=broken(rotary_dim=63)), EINVAL),
     (dict(rope=broken(rotary_dim=0)), EINVAL), (dict(rope=broken(layout=2)), EINVAL), (dict(rope=broken(n_axes=0)), EINVAL), (dict(rope=broken(n_axes=5)), EINVAL),
     (dict(rope=broken(axis=1)), EINVAL), (dict(rope=broken(freq=math.nan)), EINVAL), (dict(rope=broken(freq=1e4)), EINVAL), (dict(rope=broken(magnitude=math.inf)), EINVAL)])
 def test_rope(change, code):

@@ -134,3 +134,13 @@ def test_scaled_frequencies_reach_the_kernel():
         y = torch.empty_like(x, device=DEV)
         bs.bs_rope_apply(rope, [x.to(DEV)], [y], bs.BS_F32, 50, 128, torch.from_numpy(pos).to(DEV), stream=stream())
         check(y, rope, x, pos, False, "f32")
+
+
+def test_one_row_for_all_heads_and_tokens_and_numbers_of_numpy():
+    """Rows of x may be the same one."""
+    rope = bs.bs_rope_init(64)
+    x = draw(1, 1, 64, "f32").expand(3, 5, 64)
+    pos = np.arange(5, dtype=np.int32)[None]
+    y = torch.empty((3, 5, 64), device=DEV)
+    bs.bs_rope_apply(rope, [x[:1, :1].to(DEV).expand(3, 5, 64)], [y], bs.BS_F32, np.int64(5), np.int32(64), torch.from_numpy(pos).to(DEV), stream=stream())
+    check(y, rope, x.contiguous(), pos, False, "f32")
