@@ -107,18 +107,18 @@ __device__ inline int wave_upto(int x)
     return x;
 }
 
-__device__ inline int wave_sum(int x)
-{
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
-    return x;
-}
+__device__ inline int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_upto(x), 63); }
 
 __device__ inline int wave_max(int x)
 {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) x = max(x, __shfl_xor(x, off, 64));
-    return x;
+    // (a lane without a partner: the smallest number)
+    x = max(x, __builtin_amdgcn_update_dpp(INT32_MIN, x, 0x111, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(INT32_MIN, x, 0x112, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(INT32_MIN, x, 0x114, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(INT32_MIN, x, 0x118, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(INT32_MIN, x, 0x142, 0xa, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(INT32_MIN, x, 0x143, 0xc, 0xf, false));
+    return __builtin_amdgcn_readlane(x, 63);
 }
 
 template <int THREADS>
@@ -128,19 +128,14 @@ struct Sums { int wave[THREADS / 64]; };
 template <int THREADS>
 __device__ inline int sum_before(Sums<THREADS> &l, int x, int *total)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int upto = wave_upto(x);
     if (lane == 63) l.wave[wave] = upto;
     __syncthreads();
-    int before = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) {
-        const int n = l.wave[w];
-        before += w < wave ? n : 0;
-        all += n;
-    }
+    const int waves_upto = wave_upto(lane < THREADS / 64 ? l.wave[lane] : 0);
+    const int before = wave == 0 ? 0 : __builtin_amdgcn_readlane(waves_upto, wave - 1);
     __syncthreads();
-    *total = all;
+    *total = __builtin_amdgcn_readlane(waves_upto, 63);
     return before + upto - x;
 }
 
@@ -182,7 +177,7 @@ template <int THREADS>
 __device__ inline void next_digit(DigitLds<THREADS> &l, const int *hist, Known &k)
 {
     constexpr int EACH = kBins / THREADS;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i_digit = (32 - k.shift) / 11;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i_digit = (32 - k.shift) / 11;
     int x[EACH], mine = 0;   // from the largest digit down
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
@@ -192,9 +187,8 @@ __device__ inline void next_digit(DigitLds<THREADS> &l, const int *hist, Known &
     const int upto = wave_upto(mine);
     if (lane == 63) l.wave[i_digit][wave] = upto;
     __syncthreads();
-    int left = k.need - upto + mine;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) left -= w < wave ? l.wave[i_digit][w] : 0;
+    const int waves_upto = wave_upto(lane < THREADS / 64 ? l.wave[i_digit][lane] : 0);
+    int left = k.need - upto + mine - (wave == 0 ? 0 : __builtin_amdgcn_readlane(waves_upto, wave - 1));
     if (left > 0 && left <= mine) {
         bool found = false;
 #pragma unroll
