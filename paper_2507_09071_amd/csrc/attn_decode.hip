@@ -568,8 +568,8 @@ template <typename T, int D, bool WEIGHTS>
 __global__ __launch_bounds__(256) void decode_join(const DecodeArgs a)
 {
     constexpr int CH4 = D / 4, LANES = 256 / CH4;
-    __shared__ float4 acc[LANES][CH4];
-    __shared__ float2 ml[LANES];
+    __shared__ float4 acc[4][CH4];
+    __shared__ float2 ml[4];
     const int tid = threadIdx.x, ch = tid % CH4, p0 = tid / CH4, row = blockIdx.y;
     const int items = a.cache.n_kv_heads * a.groups;
     const Cut cut = a.cuts[blockIdx.x];
@@ -604,19 +604,33 @@ __global__ __launch_bounds__(256) void decode_join(const DecodeArgs a)
             sum.x = fmaf(y[i].x, f, sum.x); sum.y = fmaf(y[i].y, f, sum.y); sum.z = fmaf(y[i].z, f, sum.z); sum.w = fmaf(y[i].w, f, sum.w);
         }
     }
-    acc[p0][ch] = sum;
-    if (ch == 0) ml[p0] = make_float2(m, l);
+    // the parts that a wave has, across its lanes, then the waves
+    const auto across = [](auto f, float x) {
+        if constexpr (D == 64) {
+            const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+            x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        }
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    };
+    const auto larger = [](float x, float y) { return fmaxf(x, y); };
+    const auto plus = [](float x, float y) { return x + y; };
+    const float m_wave = across(larger, m), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_wave) * a.scale_log2e);
+    l = across(plus, l * f);
+    sum = make_float4(across(plus, sum.x * f), across(plus, sum.y * f), across(plus, sum.z * f), across(plus, sum.w * f));
+    if ((tid & 63) < CH4) acc[tid >> 6][ch] = sum;
+    if ((tid & 63) == 0) ml[tid >> 6] = make_float2(m_wave, l);
     __syncthreads();
-    if (p0 != 0) return;
-    float m_all = -INFINITY;
-    for (int i = 0; i < LANES; ++i) m_all = fmaxf(m_all, ml[i].x);
+    if (tid >= CH4) return;
+    const float m_all = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
     l = 0.f;
     sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = 0; i < LANES; ++i) {
-        const float f = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[i].x - m_all) * a.scale_log2e);
-        l = fmaf(ml[i].y, f, l);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float g = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[i].x - m_all) * a.scale_log2e);
         const float4 y = acc[i][ch];
-        sum.x = fmaf(y.x, f, sum.x); sum.y = fmaf(y.y, f, sum.y); sum.z = fmaf(y.z, f, sum.z); sum.w = fmaf(y.w, f, sum.w);
+        l = fmaf(ml[i].y, g, l);
+        sum.x = fmaf(y.x, g, sum.x); sum.y = fmaf(y.y, g, sum.y); sum.z = fmaf(y.z, g, sum.z); sum.w = fmaf(y.w, g, sum.w);
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     store_row4(static_cast<T *>(a.out) + seq * a.out_seq + (row0 + row) * a.out_head + 4 * ch, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
