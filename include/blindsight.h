@@ -525,8 +525,7 @@ int bs_cache_append(const bs_cache *cache, const bs_heads *k, const bs_heads *v,
  *                not looked at.  Not together with a window (BS_EUNSUPPORTED).
  *   workspace    at least bs_attn_decode_workspace bytes, 16-byte aligned
  * Slots that are not seen may hold anything, infinities and NaN too; a seen one with such a value can make the rows that see it
- * not finite.  bf16: probabilities have 16 bits before P V (two bf16 numbers each), so the result is as good as its own rounding; scores, sums
- * and weights are fp32.
+ * not finite.  Probabilities (bf16: as three bf16 numbers each), scores, sums and weights are fp32; the result is rounded once.
  * Same inputs, same bits: nothing depends on the order in which workgroups finish.
  */
 int bs_attn_decode(const bs_cache *cache, const bs_heads *q, const bs_heads *out, const int32_t *lens, int32_t window, float scale,
