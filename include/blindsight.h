@@ -480,7 +480,8 @@ int bs_rope_apply(const bs_rope *rope, const bs_heads *x, const bs_heads *y, int
 
 /* A KV cache in pages.  Slot j of sequence s and KV head h lies in page p = page_table[s * max_pages + j / page_size] at
  * k[p * page_stride + h * head_stride + (j % page_size) * slot_stride], head_dim contiguous elements, and likewise in v; strides in
- * elements and at least head_dim where the cache is written, so that [page][head][slot][d] and [page][slot][head][d] both fit.  A page number outside [0, n_pages) means that these
+ * elements; where the cache is written, its rows lie apart, the axes nested in any order (BS_EINVAL), so that [page][head][slot][d] and
+ * [page][slot][head][d] both fit, and k and v do not overlap.  A page number outside [0, n_pages) means that these
  * slots have no page: they are not written, and nobody sees them.  k and v 16-byte aligned, strides multiples of 16 bytes;
  * head_dim a multiple of 8 up to 256 (bs_attn_decode: 64 or 128), page_size a multiple of 16. */
 typedef struct {
