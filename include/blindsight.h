@@ -473,7 +473,8 @@ int bs_rope_init(bs_rope *rope, int32_t rotary_dim, int32_t layout, double base,
  *   positions  device, row a = axis a, axis_stride elements apart: positions[a * axis_stride + t], any 32-bit value
  *   flags      0 or BS_ROPE_INVERSE
  * The angle is formed and reduced in 64 bits, so far positions turn as exactly as near ones; the product is fp32, rounded
- * once.  Any alignment and stride; 16-byte loads are used where pointers, strides and sizes allow them.  n_tokens may be 0.
+ * once.  Any alignment and stride; 16-byte loads are used where pointers, strides and sizes allow them.  n_tokens may be 0, and pointers to
+ * data, positions and lists of tokens null then (as of bs_cache_append).
  */
 int bs_rope_apply(const bs_rope *rope, const bs_heads *x, const bs_heads *y, int32_t n_tensors, int32_t dtype, int32_t n_tokens,
                   int32_t head_dim, const int32_t *positions, int64_t axis_stride, uint32_t flags, void *stream);

@@ -15,7 +15,7 @@ constexpr int64_t kMaxSlots = INT32_MAX - 65536;
 constexpr int64_t kMaxStride = (int64_t)1 << 40;
 
 int check_cache(const bs_cache *c);
-int check_heads(const bs_heads *h);   // data, sizes and strides
+int check_heads(const bs_heads *h, bool none = false);   // data, sizes and strides; none: of no tokens, whose data may be null
 // Rows that are written lie apart from each other.
 int check_rows_apart(const bs_heads &h, int32_t n_tokens, int32_t head_dim);
 int check_rows_apart(const bs_cache &c);

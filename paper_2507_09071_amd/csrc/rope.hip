@@ -32,9 +32,9 @@ int check_cache(const bs_cache *c)
     return BS_OK;
 }
 
-int check_heads(const bs_heads *h)
+int check_heads(const bs_heads *h, bool none)
 {
-    if (!h || !h->data || h->n_heads <= 0 || h->head_stride < 0 || h->token_stride < 0 || h->head_stride > kMaxStride || h->token_stride > kMaxStride) return BS_EINVAL;
+    if (!h || (!h->data && !none) || h->n_heads <= 0 || h->head_stride < 0 || h->token_stride < 0 || h->head_stride > kMaxStride || h->token_stride > kMaxStride) return BS_EINVAL;
     return BS_OK;
 }
 
@@ -263,9 +263,9 @@ int run_rope(RopeArgs &a, const bs_rope *rope, int32_t dtype, int32_t head_dim, 
     return err == hipSuccess ? BS_OK : fail_hip(err, "rope_rows launch");
 }
 
-int check_rope(const bs_rope *r, int32_t head_dim, const int32_t *positions, int64_t axis_stride)
+int check_rope(const bs_rope *r, int32_t n_tokens, int32_t head_dim, const int32_t *positions, int64_t axis_stride)
 {
-    if (!r || !positions || axis_stride < 0 || axis_stride > kMaxStride) return BS_EINVAL;
+    if (!r || (!positions && n_tokens > 0) || axis_stride < 0 || axis_stride > kMaxStride) return BS_EINVAL;
     if (r->rotary_dim < 2 || r->rotary_dim % 2 != 0 || r->rotary_dim > 2 * BS_ROPE_MAX_PAIRS || r->rotary_dim > head_dim) return BS_EINVAL;
     if ((r->layout != BS_ROPE_HALF && r->layout != BS_ROPE_INTERLEAVED) || r->n_axes < 1 || r->n_axes > BS_ROPE_MAX_AXES) return BS_EINVAL;
     if (!std::isfinite(r->magnitude)) return BS_EINVAL;
@@ -329,12 +329,12 @@ extern "C" int bs_rope_apply(const bs_rope *rope, const bs_heads *x, const bs_he
     using namespace bs;
     if (!x || !y || n_tensors < 1 || n_tensors > 2 || n_tokens < 0 || (flags & ~BS_ROPE_INVERSE)) return BS_EINVAL;
     if (head_dim < 2 || head_dim % 2 != 0 || head_dim > 2 * BS_ROPE_MAX_PAIRS) return BS_EINVAL;
-    if (int rc = check_rope(rope, head_dim, positions, axis_stride)) return rc;
+    if (int rc = check_rope(rope, n_tokens, head_dim, positions, axis_stride)) return rc;
     if (dtype != BS_BF16 && dtype != BS_F32) return BS_EUNSUPPORTED;
     RopeArgs a{};
     a.n_jobs = n_tensors;
     for (int i = 0; i < n_tensors; ++i) {
-        if (check_heads(&x[i]) || check_heads(&y[i]) || x[i].n_heads != y[i].n_heads || x[i].n_heads > (1 << 20)) return BS_EINVAL;
+        if (check_heads(&x[i], n_tokens == 0) || check_heads(&y[i], n_tokens == 0) || x[i].n_heads != y[i].n_heads || x[i].n_heads > (1 << 20)) return BS_EINVAL;
         if (((uintptr_t)x[i].data | (uintptr_t)y[i].data) % element_bytes(dtype) != 0 || check_rows_apart(y[i], n_tokens, head_dim)) return BS_EINVAL;
         a.jobs[i] = job_of(x[i], y[i], true);
     }
@@ -350,12 +350,12 @@ extern "C" int bs_cache_append(const bs_cache *cache, const bs_heads *k, const b
 {
     using namespace bs;
     if (int rc = check_cache(cache)) return rc;
-    if (check_heads(k) || check_heads(v) || !token_slot || n_tokens < 0) return BS_EINVAL;
+    if (n_tokens < 0 || check_heads(k, n_tokens == 0) || check_heads(v, n_tokens == 0) || (!token_slot && n_tokens > 0)) return BS_EINVAL;
     if (k->n_heads != cache->n_kv_heads || v->n_heads != cache->n_kv_heads || !q != !q_out || (q && !rope)) return BS_EINVAL;
-    if (q && (check_heads(q) || check_heads(q_out) || q->n_heads != q_out->n_heads || q->n_heads > (1 << 20) || check_rows_apart(*q_out, n_tokens, cache->head_dim))) return BS_EINVAL;
+    if (q && (check_heads(q, n_tokens == 0) || check_heads(q_out, n_tokens == 0) || q->n_heads != q_out->n_heads || q->n_heads > (1 << 20) || check_rows_apart(*q_out, n_tokens, cache->head_dim))) return BS_EINVAL;
     if (int rc = check_rows_apart(*cache)) return rc;
     if (rope)
-        if (int rc = check_rope(rope, cache->head_dim, positions, axis_stride)) return rc;
+        if (int rc = check_rope(rope, n_tokens, cache->head_dim, positions, axis_stride)) return rc;
     if (slots)
         if (int rc = check_slots(*cache, slots)) return rc;
     const int e = element_bytes(cache->dtype);
