@@ -8,6 +8,7 @@ fails loudly — there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import struct
 
@@ -437,15 +438,53 @@ class Heads(ctypes.Structure):
 _pack_heads = struct.Struct("=QqqiI").pack   # the layout of bs_heads
 
 
-def _heads(x) -> bytes:
+def _heads(x, n_tokens: int = 0, head_dim: int = 0, item: int = 0) -> bytes:
     """A bs_heads of a tensor (or Heads), as bytes: a call for q and k needs four, and structures took longer to make than the rotation of a few
-    tokens takes (8 tokens, a pass: 10.4 -> 9.1 us)."""
-    if isinstance(x, Heads):
-        return bytes(x)
-    head, token, channel = x.stride()
+    tokens takes (8 tokens, a pass: 10.4 -> 9.1 us).  The tensor has to hold n_tokens rows of head_dim elements of `item` bytes (0: any); what a
+    Heads points to is the caller's to know."""
+    try:
+        head, token, channel = x.stride()
+    except AttributeError:
+        if isinstance(x, Heads):
+            return bytes(x)
+        raise
+    n_heads, tokens, channels = x.shape
     if channel != 1:
         raise ValueError("the channels of a head have to be contiguous")
-    return _pack_heads(x.data_ptr(), head, token, x.shape[0], 0)
+    if tokens < n_tokens or channels < head_dim or (item and x.element_size() != item):
+        raise ValueError(f"heads of shape {tuple(x.shape)} and {x.element_size()} bytes an element, where the call has {n_tokens} tokens, {head_dim} channels, {item} bytes")
+    return _pack_heads(x.data_ptr(), head, token, n_heads, 0)
+
+
+_ITEM = {BS_BF16: 2, BS_F32: 4}   # bytes; another dtype is the library's to refuse
+
+
+def _ints(x, n: int, name: str):
+    """Address of at least n whole numbers of 32 bits, one behind the other (a tensor, an address, or None)."""
+    try:
+        fits = x.element_size() == 4 and x.numel() >= n and x.is_contiguous()
+    except AttributeError:
+        return None if x is None else int(x)
+    if not fits:
+        raise ValueError(f"{name} has to be contiguous int32, {n} numbers")
+    return x.data_ptr()
+
+
+def _positions(x, n_axes: int, n_tokens: int, axis_stride: int):
+    """Address of positions: n_axes rows of n_tokens numbers of 32 bits, axis_stride apart."""
+    need = (n_axes - 1) * axis_stride + n_tokens if n_tokens else 0
+    try:
+        item = x.element_size()
+    except AttributeError:
+        return None if x is None else int(x)
+    if item != 4:
+        raise ValueError("positions have to be int32")
+    if x.numel() < need or not x.is_contiguous():
+        # a part of a larger array: rows behind the first one may lie outside the view, but within the array
+        view = x.dim() > 0 and x.stride()[-1] == 1 and x.shape[-1] >= n_tokens and (n_axes == 1 or x.dim() == 1 or x.stride()[-2] == axis_stride)
+        if not view or x.untyped_storage().nbytes() // 4 - x.storage_offset() < need:
+            raise ValueError(f"positions do not hold {n_axes} rows of {n_tokens} numbers, {axis_stride} apart")
+    return x.data_ptr()
 
 
 class KVCache(ctypes.Structure):
@@ -473,22 +512,31 @@ class KVCache(ctypes.Structure):
 class CacheSlots(ctypes.Structure):
     """bs_slots: the attention that every slot has received and the running number of its token."""
     _fields_ = [("weights", ctypes.c_void_p), ("order", ctypes.c_void_p), ("row_stride", ctypes.c_int64)]
+    rows = None   # that the arrays have; of addresses alone the caller knows
 
     @classmethod
     def of(cls, weights=None, order=None) -> "CacheSlots":
         """weights: float32, order: int32, contiguous [n_seqs, n_kv_heads, slots] (either may be left out)."""
-        strides = {x.shape[-1] for x in (weights, order) if x is not None}
-        if len(strides) != 1 or not all(x is None or (x.is_contiguous() and x.element_size() == 4) for x in (weights, order)):
-            raise ValueError("weights and order have to be contiguous, of 32 bits and of one shape")
-        return cls(None if weights is None else weights.data_ptr(), None if order is None else order.data_ptr(), strides.pop())
+        shapes = {tuple(x.shape) for x in (weights, order) if x is not None}
+        if len(shapes) != 1 or not all(x is None or (x.is_contiguous() and x.element_size() == 4 and x.is_floating_point() == f) for x, f in ((weights, True), (order, False))):
+            raise ValueError("weights (float32) and order (int32) have to be contiguous and of one shape")
+        *rows, stride = shapes.pop()
+        slots = cls(None if weights is None else weights.data_ptr(), None if order is None else order.data_ptr(), stride)
+        slots.rows = math.prod(rows)
+        return slots
 
 
 def _ref(x):
     return None if x is None else ctypes.byref(x)
 
 
-def _address(x):
-    return None if x is None else _ptr(x)
+def _slots_ref(slots, cache: KVCache):
+    if slots is None:
+        return None
+    rows = slots.rows
+    if rows is not None and rows < cache.n_seqs * cache.n_kv_heads:
+        raise ValueError(f"weights and order have {rows} rows, the cache {cache.n_seqs} sequences of {cache.n_kv_heads} heads")
+    return ctypes.byref(slots)
 
 
 def bs_rope_init(rotary_dim: int, layout: int = BS_ROPE_HALF, base: float = 1e4, scaling: int = BS_ROPE_PLAIN, factor: float = 1.0,
@@ -506,12 +554,13 @@ def bs_rope_apply(rope: Rope, xs, ys, dtype: int, n_tokens: int, head_dim: int, 
                   inverse: bool = False, stream=None) -> None:
     """xs, ys: one or two tensors [n_heads, n_tokens, head_dim] of any strides (or Heads), e.g. q and k; ys may be xs.  positions:
     int32 [n_axes, n_tokens] on the device, rows axis_stride apart (n_tokens by default).  inverse: the gradient.  Enqueues only."""
-    n = len(xs)
+    n, n_tokens, head_dim = len(xs), int(n_tokens), int(head_dim)
     if len(ys) != n:
         raise ValueError("as many ys as xs")
-    rc = load_library().bs_rope_apply(ctypes.byref(rope), b"".join(map(_heads, xs)), b"".join(map(_heads, ys)), n, int(dtype), int(n_tokens),
-                                      int(head_dim), _ptr(positions), int(n_tokens if axis_stride is None else axis_stride),
-                                      BS_ROPE_INVERSE if inverse else 0, int(stream) if stream else None)
+    item, step = _ITEM.get(dtype, 0), n_tokens if axis_stride is None else int(axis_stride)
+    rc = load_library().bs_rope_apply(ctypes.byref(rope), b"".join([_heads(x, n_tokens, head_dim, item) for x in xs]),
+                                      b"".join([_heads(y, n_tokens, head_dim, item) for y in ys]), n, int(dtype), n_tokens, head_dim,
+                                      _positions(positions, rope.n_axes, n_tokens, step), step, BS_ROPE_INVERSE if inverse else 0, int(stream) if stream else None)
     _check(rc, "bs_rope_apply")
 
 
@@ -519,9 +568,14 @@ def bs_cache_append(cache: KVCache, k, v, n_tokens: int, token_seq, token_slot, 
                     axis_stride: int | None = None, q=None, q_out=None, slots: CacheSlots | None = None, token_order=None, stream=None) -> None:
     """k, v, q, q_out: tensors [n_heads, n_tokens, head_dim] of any strides (or Heads); token_seq (None: token t is of sequence t),
     token_slot, token_order (None: the slot's number): int32 on the device.  Enqueues only."""
-    rc = load_library().bs_cache_append(ctypes.byref(cache), _heads(k), _heads(v), int(n_tokens), _address(token_seq), _ptr(token_slot), _ref(rope),
-                                        _address(positions), int(n_tokens if axis_stride is None else axis_stride), None if q is None else _heads(q),
-                                        None if q_out is None else _heads(q_out), _ref(slots), _address(token_order), int(stream) if stream else None)
+    n_tokens = int(n_tokens)
+    d, item, step = cache.head_dim, _ITEM.get(cache.dtype, 0), n_tokens if axis_stride is None else int(axis_stride)
+    rc = load_library().bs_cache_append(ctypes.byref(cache), _heads(k, n_tokens, d, item), _heads(v, n_tokens, d, item), n_tokens,
+                                        None if token_seq is None else _ints(token_seq, n_tokens, "token_seq"), _ints(token_slot, n_tokens, "token_slot"), _ref(rope),
+                                        None if rope is None else _positions(positions, rope.n_axes, n_tokens, step), step,
+                                        None if q is None else _heads(q, n_tokens, d, item), None if q_out is None else _heads(q_out, n_tokens, d, item),
+                                        _slots_ref(slots, cache), None if token_order is None else _ints(token_order, n_tokens, "token_order"),
+                                        int(stream) if stream else None)
     _check(rc, "bs_cache_append")
 
 
@@ -537,8 +591,9 @@ def bs_attn_decode(cache: KVCache, q, out, lens, scale: float, workspace, window
                    slots_out: CacheSlots | None = None, stream=None) -> None:
     """q, out: tensors [n_q_heads, n_seqs, head_dim] of any strides (or Heads); lens: int32 [n_seqs] on the device; workspace: a tensor, or
     (address, bytes), of bs_attn_decode_workspace bytes.  slots, slots_out: add up the attention that every slot receives.  Enqueues only."""
-    rc = load_library().bs_attn_decode(ctypes.byref(cache), _heads(q), _heads(out), _ptr(lens), int(window), float(scale), _ref(slots),
-                                       _ref(slots_out), *_buffer(workspace), int(stream) if stream else None)
+    n_seqs, d, item = cache.n_seqs, cache.head_dim, _ITEM.get(cache.dtype, 0)
+    rc = load_library().bs_attn_decode(ctypes.byref(cache), _heads(q, n_seqs, d, item), _heads(out, n_seqs, d, item), _ints(lens, n_seqs, "lens"), int(window), float(scale),
+                                       _slots_ref(slots, cache), _slots_ref(slots_out, cache), *_buffer(workspace), int(stream) if stream else None)
     _check(rc, "bs_attn_decode")
 
 
@@ -553,8 +608,9 @@ def bs_cache_evict(cache: KVCache, lens, lens_out, keep: int, keep_first: int, k
                    stream=None) -> None:
     """lens, lens_out: int32 [n_seqs] on the device, may be the same, as slots and slots_out; workspace: a tensor, or (address, bytes), of
     bs_cache_evict_workspace bytes.  Enqueues only."""
-    rc = load_library().bs_cache_evict(ctypes.byref(cache), _ptr(lens), _ptr(lens_out), int(keep), int(keep_first), int(keep_last), _ref(slots),
-                                       _ref(slots_out), *_buffer(workspace), int(stream) if stream else None)
+    n_seqs = cache.n_seqs
+    rc = load_library().bs_cache_evict(ctypes.byref(cache), _ints(lens, n_seqs, "lens"), _ints(lens_out, n_seqs, "lens_out"), int(keep), int(keep_first), int(keep_last),
+                                       _slots_ref(slots, cache), _slots_ref(slots_out, cache), *_buffer(workspace), int(stream) if stream else None)
     _check(rc, "bs_cache_evict")
 
 
