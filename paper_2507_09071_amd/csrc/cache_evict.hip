@@ -648,6 +648,9 @@ int check_evict(const bs_cache *cache, int32_t keep)
     if (int rc = check_cache(cache)) return rc;
     if (int rc = check_rows_apart(*cache)) return rc;
     if (keep < 1) return BS_EINVAL;
+    // A grid has fewer than 2^32 threads (see launch_select), with which sizes of the workspace stay within 64 bits.
+    const int64_t capacity = cache_slots(*cache), threads = capacity > kRanksMax || capacity <= 8 * 256 ? 256 : capacity <= 16 * 512 ? 512 : 1024;
+    if ((int64_t)cache->n_seqs * cache->n_kv_heads * threads > UINT32_MAX) return BS_EUNSUPPORTED;
     return BS_OK;
 }
 
