@@ -544,7 +544,11 @@ int64_t bs_attn_decode_workspace(const bs_cache *cache, int32_t n_q_heads, int32
  * that the first two are more than `keep`: the lowest of these slots.)
  * Kept slots at or behind `keep` move into the evicted slots before it, the first into the first, and so on, K, V, weight and order
  * alike; all other slots stay where they are.  (So as few as can be move: a row cut back from 4160 slots to 4096 moves at most 64.  Keys
- * carry their positions, attention does not mind the order.)  A slot without a page moves its weight and order alone.
+ * carry their positions, attention does not mind the order.)
+ * A sequence that is cut back (lens[s] > keep) needs a page for every slot below lens[s]; others may lack some.  (Page numbers are on the device, so
+ * this cannot be refused.  A slot without a page is ranked like any other, and only its weight and order move: a token that moves into it is
+ * lost, and a hole that it moves into shows the evicted token's K and V under its name.  So a sequence whose first pages were given back, behind
+ * a window, is not one to cut back.  Nothing outside the cache is touched in any case.)
  *   lens, lens_out     device [n_seqs]: slots in use (held within [0, max_pages * page_size]), and min(lens, keep); may be the same
  *   slots, slots_out   weights and order before and after; entries from lens_out on are not touched; may be the same, else they do not
  *                      overlap

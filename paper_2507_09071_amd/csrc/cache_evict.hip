@@ -242,7 +242,7 @@ __device__ inline void do_moves(const EvictArgs &a, int row, unsigned n)
         const float w = a.weights[row * a.in_stride + src];
         const int32_t o = a.order[row * a.in_stride + src];
         const int64_t d = slot_offset(a.cache, seq, head, dst), s = slot_offset(a.cache, seq, head, src);
-        to[tid] = d < 0 || s < 0 ? -1 : d * bytes;
+        to[tid] = d < 0 || s < 0 ? -1 : d * bytes;   // (the caller sees to it that both have a page)
         from[tid] = s * bytes;
         a.weights_out[row * a.out_stride + dst] = w;
         a.order_out[row * a.out_stride + dst] = o;
