@@ -272,6 +272,9 @@ __device__ inline void do_moves(const EvictArgs &a, int row, unsigned n)
 // ------------------------------------------------------------------------------------ one workgroup per row
 
 constexpr int kRanksMax = 32768;   // 128 KB of LDS
+// Beside them: three histograms, what is known of the digits, sums, a count of each 64 slots, the newest order, the moves.
+static_assert(kRanksMax * 4 + kDigits * kBins * 4 + sizeof(DigitLds<1024>) + sizeof(Sums<1024>) + kRanksMax / 64 * 4 + 4 + kMovesAtOnce * 16 <= 160 * 1024 - 64, "LDS of a CU");
+static_assert(kRanksMax <= 32768, "kept slots and ties are counted in 16 bits each");
 
 // SLOTS > 0: a thread has at most so many slots and keeps them in registers.  Else ranks lie in LDS, and orders and weights are read again.
 template <int THREADS, int SLOTS>
