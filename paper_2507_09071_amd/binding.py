@@ -440,7 +440,7 @@ _pack_heads = struct.Struct("=QqqiI").pack   # the layout of bs_heads
 
 def _heads(x, n_tokens: int = 0, head_dim: int = 0, item: int = 0) -> bytes:
     """A bs_heads of a tensor (or Heads), as bytes: a call for q and k needs four, and structures took longer to make than the rotation of a few
-    tokens takes (8 tokens, a pass: 10.4 -> 9.1 us).  The tensor has to hold n_tokens rows of head_dim elements of `item` bytes (0: any); what a
+    tokens takes (8 tokens, a pass: 10.4 -> 9.1 us; 0.6 more with the checks).  The tensor has to hold n_tokens rows of head_dim elements of `item` bytes (0: any); what a
     Heads points to is the caller's to know."""
     try:
         head, token, channel = x.stride()

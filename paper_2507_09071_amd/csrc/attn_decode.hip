@@ -1,12 +1,13 @@
 // Attention of one new token per sequence over a paged cache.
 //
 // What has to be done is reading K and V of every visible slot once, so the bound is HBM: 4 d FLOP for every query head of a group
-// and slot are at most a few dozen per byte, which the matrix pipe does on the side (busy 6 % of the time).  Measured: two sequences of 150K
-// slots, 32 / 16 heads of 128, 2.46 GB: 412 us, 6.0 TB/s, what a kernel that only reads reaches; one of 39.5K, 28 / 4 heads, 81 MB: 23.4 us, of
-// which the two kernels are 17.4 and 4.0 (13 at that rate); 48 sequences of 17 to 16K slots, 40 / 8 heads, 498 MB: 102 us; fp32, 32 / 8 heads, four
-// sequences of 8K to 16K: 77 us, 5.0 TB/s.  Tried: half as many waves in twice as many workgroups (412 -> 448), a wave per short item (256 sequences of
-// 5 to 300 slots, two heads a group: 70 -> 56, but 200 of 200 to 2K 70 -> 72 and more), query rows and page numbers of the next item ahead of
-// time (nothing).  How:
+// and slot are at most a few dozen per byte, which the matrix pipe does on the side (busy 7 % of the time).  Measured: two sequences of 150K
+// slots, 32 / 16 heads of 128, 2.46 GB: 412 us, 6.0 TB/s, what a kernel that only reads reaches; one of 39.5K, 28 / 4 heads, 81 MB: 21 to 24 us, of
+// which the two kernels are 17.8 and 4.0 (13 at that rate); 48 sequences of 17 to 16K slots, 40 / 8 heads, 498 MB: 102 us; fp32, 32 / 8 heads, four
+// sequences of 8K to 16K: 76 us, 5.0 TB/s.  Farthest from that rate are many short sequences, whose items are two or three blocks for four waves, with an
+// empty pipeline and a merge around each: 256 of 5 to 300 slots, 32 / 16 heads, 161 MB: 73 us (26 at that rate), 40 / 8 heads, 84 MB: 44 (13).
+// Tried: half as many waves in twice as many workgroups (412 -> 448), a wave per short item (the 73 us 70 -> 56 before probabilities were whole, but
+// 3 % and more slower where sequences have 200 to 2K slots), query rows and page numbers of the next item ahead of time (nothing).  How:
 //  * the query heads of a KV head are the free dimension of a 16x16 MFMA (one block of 16 rows, or two; groups of 32 beyond that), so K and
 //    V are read once for all of them;
 //  * the work of all sequences and KV heads ("items") is one row of blocks of 32 slots (16 in fp32: the same bytes), cut into equal
@@ -14,7 +15,8 @@
 //    sum over the lengths.  A batch of very different lengths is balanced to within four blocks, and one long sequence fills the chip;
 //  * the four waves of a workgroup take every fourth block and run on their own: no barrier in the loop.  K and V blocks go from
 //    the pages to LDS with 16-byte LDS-direct loads, two blocks deep: 32 KB in flight per wave.  Page numbers come through the scalar cache,
-//    a step before they are needed.  Chunks of 16 bytes are exchanged within a row (XOR with its number) so that column reads are free of conflicts;
+//    a step before they are needed.  Chunks of 16 bytes are exchanged within a row (XOR with its number) so that reads of K's columns are free of conflicts; of V two
+//    rows meet in the same banks (two cycles more a read, 16 of 24 reads of a block), which does not show while memory is the bound;
 //  * an item that lies within a share is finished there, another's parts are joined by a second, small kernel in a fixed order;
 //  * with weights, the scores are left in the workspace (4 bytes per head and slot, where K has 256) and a third kernel turns them
 //    into probabilities once the sums are known: reading K again would cost half as much as the attention.
@@ -78,7 +80,7 @@ struct Traits {
 };
 
 // Beginning an item (its query rows, an empty pipeline, the merge of the waves) costs about as much as so many blocks: shares are equal with
-// that counted.  Else a share of many short sequences takes longest: 48 sequences of 17 to 16K slots 100 us, 123 without.
+// that counted.  Else a share of many short sequences takes longest: 48 sequences of 17 to 16K slots 102 us, 130 without.
 constexpr int kItemBlocks = 4;
 
 // Blocks of a sequence that are visible, from block `first` on; `units`: those of an item and what its beginning costs.
@@ -225,7 +227,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void decode_shares(const
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(newer)::value) : "memory");
     };
     const auto reads_done = []() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
-    // Stores of scores count among the loads in flight.  Those of the second row block are not counted: there may be none.  (What they cost, 412 -> 475
+    // Stores of scores count among the loads in flight.  Those of the second row block are not counted: there may be none.  (What they cost, 412 -> 475 to 500
     // us for two sequences of 150K slots with two heads a group, is the same with half as many, with four blocks' together, past the caches, and to a
     // few lines over and over: memory turns around for them.)
     constexpr int NS = WEIGHTS ? SUB : 0;

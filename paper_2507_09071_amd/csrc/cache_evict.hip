@@ -5,11 +5,13 @@
 // ties go to the lowest slots.  The first digit is sign, exponent and two bits of the fraction, over which weights spread well, so that few
 // lanes of a wave count in the same place; mostly the second one leaves no more slots than are needed, and the third is not looked at.
 // Kept slots behind `keep` move into the holes before it: the two sets do not overlap, so moves need no order among each other, and nothing
-// moves that can stay.  Weights and orders are read once or twice (8 bytes a slot), moves cost 4 rows each.
+// moves that can stay.  A workgroup that has a row reads weights and orders (8 bytes a slot) once if they fit its registers, else the
+// orders up to three times and the weights twice; in chunks every launch that ranks slots reads both again, up to five and four times.  Moves cost 4 rows each.
 //
 // Two ways to select.  One workgroup per row with the row's ranks in registers or LDS: one launch, all the chip where there are many rows.  Or a row
 // cut into chunks for many workgroups, with a launch per pass: few long rows.  Bound: latency and vector instructions of counts and scans (512 rows of
-// 4160 slots, 67 MB: 26 us, at a copy's rate 13), not memory; 4 rows of 39.5K, seven launches: 32 to 35 us.
+// 4160 slots, 67 MB: 26 to 28 us, at a copy's rate 13), not memory; 4 rows of 39.5K, seven launches: 33 to 35 us (5.4).  Lengths are on the device, so
+// the table's slots decide: those 512 rows take 28 us in a table of 4160 or 8192 slots, 36 in one of 32768 and 64 in one of 131072.
 #include <algorithm>
 #include <mutex>
 
@@ -672,12 +674,12 @@ Plan make_plan(const bs_cache &c, int32_t keep)
     p.rows = (int64_t)c.n_seqs * c.n_kv_heads;
     p.moves = std::max<int64_t>(0, std::min<int64_t>(keep, capacity - keep));
     // Rows beyond what LDS holds, and few long ones, whose CUs would be too few.  Cut back to half, a workgroup each / in chunks: 4 rows of 8K slots
-    // 17.9 / 32.1 us, of 16K 30.3 / 33.6, of 30K 50.9 / 37.1; 32 rows 32.5 / 48.0, 59.7 / 65.2, 102 / 94.
+    // 15.8 / 29.6 us, of 16K 29.0 / 31.4, of 30K 49.4 / 34.8; 32 rows 29.8 / 45.6, 58.4 / 62.9, 101 / 92.
     if (capacity > kRanksMax || (p.rows <= 32 && capacity > 20480)) {
         p.chunks = (int32_t)std::max<int64_t>(1, std::min<int64_t>({64, (capacity + 1023) / 1024, (1024 + p.rows - 1) / p.rows}));
         p.words = (int32_t)((capacity + 63) / 64);
     }
-    p.at_once = p.chunks == 0 && p.moves <= kMovesAtOnce;   // (512 rows of 4160 slots, 64 moves: 34.2 us with a kernel for the moves, 31.0 so)
+    p.at_once = p.chunks == 0 && p.moves <= kMovesAtOnce;   // (512 rows of 4160 slots, 64 moves: 31.4 us with a kernel for the moves, 28.0 so)
     const auto whole = [](int64_t bytes) { return (bytes + 255) / 256 * 256; };
     p.at_moves = whole(p.rows * 4);
     p.at_need = p.at_moves + whole(p.rows * p.moves * 8);
@@ -713,7 +715,7 @@ hipError_t launch_select(const EvictArgs &a, const Plan &p, hipStream_t st)
     if (p.chunks == 0) {
         const dim3 grid((unsigned)p.rows);
         // Eight slots a thread; more only where there are more rows than CUs, which then share one: what a wave does besides its slots (scans,
-        // barriers) counts.  Rows of 4160 slots, with 1024 threads / 512 of 16 slots: 512 rows 39.9 / 31.0 us, 128 of 8000 22.8 / 28.1.
+        // barriers) counts.  Rows of 4160 slots, with 1024 threads / 512 of 16 slots: 512 rows 34.1 / 28.0 us, 128 of 8000 20.1 / 24.6.
         if (capacity <= 8 * 256) return launch_kernel(evict_select<256, 8>, grid, dim3(256), 0, st, a);
         if (capacity <= 8 * 512) return launch_kernel(evict_select<512, 8>, grid, dim3(512), 0, st, a);
         if (capacity <= 8 * 1024 && p.rows <= 256) return launch_kernel(evict_select<1024, 8>, grid, dim3(1024), 0, st, a);

@@ -3,7 +3,8 @@
 // A pair (a, b) of channels is turned by the angle position * f: (a cos - b sin, b cos + a sin).  The work is reading every row once
 // and writing it once, so the bound is HBM, and what an angle costs has to be paid once per token and pair, not once per head: a thread keeps its
 // angles over the heads.  39.5K tokens of 28 + 4 heads, 648 MB: 124 us, 5.2 TB/s, a large copy's rate (5.0 to 5.5); the same into pages, token-major
-// rows, 730 MB: 154 us, 4.75 TB/s.  (Stores past the caches: 121 and 151 us, but 50 -> 67 for rows of which an instruction writes half a line.)
+// rows, 730 MB: 154 us, 4.75 TB/s.  Where the pairs do not divide into pieces of 16 bytes, smaller ones cost: 36 of 128 channels, pieces of 4 bytes, 136 us
+// (647 MB; at a copy's rate 122), 20 of 64 79 (61).  (Stores past the caches: 121 and 151 us, but 50 -> 67 for rows of which an instruction writes half a line.)
 #include <algorithm>
 #include <array>
 #include <cmath>
@@ -111,7 +112,8 @@ template <typename T, int V>
 struct __align__(sizeof(T) * V) Vec { T x[V]; };
 
 // cos and sin of position * quarter_turns * (pi / 2): the multiple of a quarter turn is taken off in 64 bits, and the rest, at most
-// half a quarter turn, goes through the series of sine and cosine, whose first term left out is below 2e-9 (sine) and 1e-10 (cosine).
+// half a quarter turn, goes through the series of sine and cosine in fp32: the first term left out is below 1.8e-9 (sine) and 1.2e-10 (cosine), what fp32
+// rounds on the way is up to 6.6e-8, about 2^-24.  The 64-bit angle is off by at most 3 |angle| 2^-53: 1e-9 at three million radians, 7e-7 at 2^31.
 __device__ inline void rotation(double quarter_turns, int32_t position, float &c, float &s)
 {
     const double t = quarter_turns * (double)position, n = rint(t);
