@@ -516,6 +516,45 @@ int bs_cache_append(const bs_cache *cache, const bs_heads *k, const bs_heads *v,
                     const int32_t *token_slot, const bs_rope *rope, const int32_t *positions, int64_t axis_stride, const bs_heads *q,
                     const bs_heads *q_out, const bs_slots *slots, const int32_t *token_order, void *stream);
 
+/* Root-mean-square norm of every head's d channels: x -> x (mean x^2 + eps)^-1/2 (weight + offset).  Squares and sums are fp32, so channels
+ * beyond 10^18 overflow. */
+typedef struct {
+    const void *weight[2];   /* device, [head_dim] each: of the first and the second tensor of a call (bs_cache_append_norm: of q, of k); NULL: ones, without the offset */
+    int32_t weight_dtype;    /* BS_BF16 or BS_F32, both alike; any alignment of their elements */
+    float eps;               /* > 0 (at least the smallest normal fp32 number) */
+    float offset;            /* 0, or 1 where a model keeps its weights less one */
+} bs_norm;
+
+/*
+ * Norm of every head and the rotary positions behind it in one pass: bs_rope_apply of the normed rows, which are not rounded in between.
+ * Arguments as those of bs_rope_apply; rope NULL: no rotation (positions are not looked at then).  y may be x.
+ */
+int bs_norm_rope(const bs_norm *norm, const bs_rope *rope, const bs_heads *x, const bs_heads *y, int32_t n_tensors, int32_t dtype, int32_t n_tokens,
+                 int32_t head_dim, const int32_t *positions, int64_t axis_stride, void *stream);
+
+/*
+ * Its gradient: from x and dy (the gradient of y) dx, and dweight [n_tensors][head_dim] in fp32, the sum over all heads and tokens (NULL: not wanted; it is
+ * written, not added to; of no tokens it is zero).  Nothing is kept from the way there.
+ *   dx           as many heads as x; may be x or dy (same data and strides), else it does not overlap them; rows of dx lie apart, those of x and dy may be
+ *                the same one (stride 0)
+ *   workspace    at least bs_norm_rope_grad_workspace bytes, 16-byte aligned; not looked at if dweight is NULL
+ * Same inputs, same bits.
+ */
+int bs_norm_rope_grad(const bs_norm *norm, const bs_rope *rope, const bs_heads *x, const bs_heads *dy, const bs_heads *dx, float *dweight, int32_t n_tensors,
+                      int32_t dtype, int32_t n_tokens, int32_t head_dim, const int32_t *positions, int64_t axis_stride, void *workspace, int64_t workspace_bytes,
+                      void *stream);
+
+/* Bytes of workspace of bs_norm_rope_grad (at most 4 MB); a negative error code for arguments that the call would refuse. */
+int64_t bs_norm_rope_grad_workspace(int32_t n_tensors, int32_t dtype, int32_t n_tokens, int32_t head_dim);
+
+/*
+ * bs_cache_append with norms: K goes into the cache normed with norm->weight[1] and rotated if `rope` is not NULL, V as it is; q of the same step is normed with
+ * norm->weight[0] and rotated likewise.  All else as of bs_cache_append, but q may come without a rope.
+ */
+int bs_cache_append_norm(const bs_cache *cache, const bs_heads *k, const bs_heads *v, int32_t n_tokens, const int32_t *token_seq, const int32_t *token_slot,
+                         const bs_norm *norm, const bs_rope *rope, const int32_t *positions, int64_t axis_stride, const bs_heads *q, const bs_heads *q_out,
+                         const bs_slots *slots, const int32_t *token_order, void *stream);
+
 /*
  * Attention of one new token per sequence over the cache, its own slot included:
  *   out[s, h, :] = sum_j softmax_j( scale * <q[s, h], K[s, h / G, j]> ) * V[s, h / G, j, :],  G = n_q_heads / n_kv_heads,
@@ -539,6 +578,49 @@ int bs_attn_decode(const bs_cache *cache, const bs_heads *q, const bs_heads *out
  * weights the scores of every slot that the page table has room for: 4 n_seqs n_q_heads max_pages page_size bytes and some (48 sequences, 40 heads, a table of
  * 131072 slots: 1.0 GB; of 16384: 0.13), else a few MB at most. */
 int64_t bs_attn_decode_workspace(const bs_cache *cache, int32_t n_q_heads, int32_t with_weights);
+
+#define BS_TREE_MAX_TOKENS 256
+
+/*
+ * Attention of a few drafted tokens per sequence over the cache, their own slots included.  The drafted tokens of a sequence may be a tree, several guesses at
+ * what comes next: each sees the sequence and those of the drafted tokens that its mask names.
+ *   out[t, h, :] = sum_j softmax_j( f(scale * <q[t, h], K[s, h / G, j]>) ) * V[s, h / G, j, :],  G = n_q_heads / n_kv_heads,  f(x) = x, or with cap > 0 cap tanh(x / cap)
+ *   q, out       n_q_heads heads of n_tokens tokens in the cache's dtype, 16-byte aligned, strides multiples of 16 bytes; n_q_heads a multiple of n_kv_heads; out
+ *                does not overlap q
+ *   first        device [n_seqs + 1], ascending: tokens first[s] .. first[s + 1] - 1 are sequence s's; a sequence may have none.  Tokens that no sequence has, and those of a sequence behind its
+ *                max_tokens-th, are left as they were.  (Values are held within [0, n_tokens].)
+ *   lens         device [n_seqs]: slots in use before the drafted tokens; held within [0, max_pages * page_size].  Drafted token i of sequence s is in slot lens[s] + i, and
+ *                a token sees all slots below lens[s].
+ *   max_tokens   most drafted tokens of a sequence, 1 .. BS_TREE_MAX_TOKENS
+ *   mask         device [n_tokens][mask_words]: bit a % 64 of word a / 64 of token t is set if it sees drafted token a of its sequence (itself is one of them).
+ *                mask_words >= max_tokens / 64, rounded up; bits of tokens that the sequence does not have mean nothing.  NULL (mask_words 0): a chain, each token sees itself
+ *                and the drafted ones before it.  A row that sees nothing is zero.
+ *   window       > 0: of the slots that a token sees by the above, only the last `window`
+ *   cap          >= 0; 0: none
+ *   workspace    at least bs_attn_tree_workspace bytes, 16-byte aligned
+ * Slots that no token sees may hold anything, infinities and NaN too, and a slot that only some see leaves the others as they are; one with such a value
+ * can make the rows that see it not finite.  Scores, sums and probabilities are fp32; bf16: each probability goes into P V as two bf16 numbers, off by at most
+ * 2^-16 of itself; the result is rounded once.  Same inputs, same bits.
+ */
+int bs_attn_tree(const bs_cache *cache, const bs_heads *q, const bs_heads *out, int32_t n_tokens, const int32_t *first, const int32_t *lens, int32_t max_tokens,
+                 const uint64_t *mask, int32_t mask_words, int32_t window, float scale, float cap, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace of bs_attn_tree for these sizes; a negative error code for arguments that the call would refuse.  Sizes decide, not lengths; at most 70 MB. */
+int64_t bs_attn_tree_workspace(const bs_cache *cache, int32_t n_q_heads, int32_t n_tokens, int32_t max_tokens);
+
+/*
+ * Keep the drafted tokens that were accepted: slot lens[s] + i takes what slot lens[s] + path[s][i] held when the call began, K, V, weight and order, for
+ * i < n_path[s], and lens_out[s] = lens[s] + n_path[s].  Other slots stay as they are, those of rejected tokens among them; they are free again.
+ *   lens, lens_out   device [n_seqs], held within [0, max_pages * page_size]; may be the same
+ *   path         device [n_seqs][max_path]: numbers of drafted tokens, in any order, one more than once too; where one is outside [0, BS_TREE_MAX_TOKENS), or either slot has
+ *                no page, that slot stays as it is
+ *   n_path       device [n_seqs], held within [0, max_path]
+ *   max_path     0 .. BS_TREE_MAX_TOKENS
+ *   slots        NULL, or weights and order (either pointer may be NULL) that move along
+ * Pages that are moved into must not be shared with other sequences.
+ */
+int bs_cache_accept(const bs_cache *cache, const int32_t *lens, int32_t *lens_out, const int32_t *path, const int32_t *n_path, int32_t max_path,
+                    const bs_slots *slots, void *stream);
 
 /*
  * Cut the cache back to `keep` slots per sequence and KV head, where it holds more.  Kept are the slots whose order is below

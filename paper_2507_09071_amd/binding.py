@@ -24,7 +24,8 @@ EXPORTS = ("bs_build_tilemap", "bs_build_tilemap_ex", "bs_build_tilemap_model", 
            "bs_attn_prefill", "bs_attn_prefill_ex", "bs_attn_prefill_static", "bs_static_scratch_bytes",
            "bs_characterize_prompt", "bs_head_sq_error", "bs_aggregate_head_type", "bs_aggregate_layer", "bs_alpha_layer",
            "bs_rope_init", "bs_rope_apply", "bs_cache_append", "bs_attn_decode", "bs_attn_decode_workspace", "bs_cache_evict",
-           "bs_cache_evict_workspace", "bs_strerror", "bs_last_error")
+           "bs_cache_evict_workspace", "bs_norm_rope", "bs_norm_rope_grad", "bs_norm_rope_grad_workspace", "bs_cache_append_norm", "bs_attn_tree",
+           "bs_attn_tree_workspace", "bs_cache_accept", "bs_strerror", "bs_last_error")
 
 
 class BlindsightError(RuntimeError):
@@ -139,6 +140,20 @@ def load_library():
     lib.bs_cache_evict.restype = ctypes.c_int
     lib.bs_cache_evict_workspace.argtypes = [vp, i32]
     lib.bs_cache_evict_workspace.restype = i64
+    lib.bs_norm_rope.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, i64, vp]
+    lib.bs_norm_rope.restype = ctypes.c_int
+    lib.bs_norm_rope_grad.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, i64, vp, i64, vp]
+    lib.bs_norm_rope_grad.restype = ctypes.c_int
+    lib.bs_norm_rope_grad_workspace.argtypes = [i32, i32, i32, i32]
+    lib.bs_norm_rope_grad_workspace.restype = i64
+    lib.bs_cache_append_norm.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp]
+    lib.bs_cache_append_norm.restype = ctypes.c_int
+    lib.bs_attn_tree.argtypes = [vp, vp, vp, i32, vp, vp, i32, vp, i32, i32, ctypes.c_float, ctypes.c_float, vp, i64, vp]
+    lib.bs_attn_tree.restype = ctypes.c_int
+    lib.bs_attn_tree_workspace.argtypes = [vp, i32, i32, i32]
+    lib.bs_attn_tree_workspace.restype = i64
+    lib.bs_cache_accept.argtypes = [vp, vp, vp, vp, vp, i32, vp, vp]
+    lib.bs_cache_accept.restype = ctypes.c_int
     lib.bs_strerror.argtypes = [ctypes.c_int]
     lib.bs_strerror.restype = ctypes.c_char_p
     lib.bs_last_error.argtypes = []
@@ -619,3 +634,148 @@ def bs_cache_evict_workspace(cache: KVCache, keep: int) -> int:
     if n < 0:
         _check(int(n), "bs_cache_evict_workspace")
     return int(n)
+
+
+# ---------------------------------------------------------------------------------------- normed heads, drafted tokens
+
+BS_TREE_MAX_TOKENS = 256
+
+
+class Norm(ctypes.Structure):
+    """bs_norm: weights of a root-mean-square norm of the heads of one or two tensors.  Holds addresses only; the caller keeps the weights alive."""
+    _fields_ = [("weight", ctypes.c_void_p * 2), ("weight_dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("offset", ctypes.c_float)]
+    sizes = (None, None)   # elements of the weights; of addresses alone the caller knows
+
+    @classmethod
+    def of(cls, weights, eps: float = 1e-6, offset: float = 0.0) -> "Norm":
+        """weights: one or two contiguous tensors [head_dim], alike in type (bfloat16 or float32), of the first and the second tensor of a call
+        (bs_cache_append_norm: of q, of k); None: ones, without the offset."""
+        weights = list(weights)
+        there = [w for w in weights if w is not None]
+        items = {(w.element_size(), w.is_floating_point()) for w in there}
+        if not 1 <= len(weights) <= 2 or len(items) > 1 or not items <= {(2, True), (4, True)} or not all(w.dim() == 1 and w.is_contiguous() for w in there):
+            raise ValueError("one or two weights, contiguous [head_dim], both bfloat16 or both float32")
+        if any(str(w.dtype).endswith("float16") and not str(w.dtype).endswith("bfloat16") for w in there):
+            raise ValueError("weights in bfloat16 or float32")
+        norm = cls((ctypes.c_void_p * 2)(*[None if w is None else w.data_ptr() for w in weights]), BS_BF16 if items == {(2, True)} else BS_F32, float(eps), float(offset))
+        norm.sizes = tuple(None if w is None else w.numel() for w in weights) + (None,) * (2 - len(weights))
+        norm.n_weights = len(weights)
+        return norm
+
+    n_weights = 2
+
+
+def _norm_ref(norm: Norm, head_dim: int, first: int, last: int):
+    """Of the weights that a call with heads of head_dim channels looks at: numbers first .. last."""
+    if last >= norm.n_weights:
+        raise ValueError("a weight, or None, for each tensor")
+    for n in norm.sizes[first:last + 1]:
+        if n is not None and n != head_dim:
+            raise ValueError(f"a weight of {n} channels, where the heads have {head_dim}")
+    return ctypes.byref(norm)
+
+
+def bs_norm_rope(norm: Norm, rope: Rope | None, xs, ys, dtype: int, n_tokens: int, head_dim: int, positions=None, axis_stride: int | None = None, stream=None) -> None:
+    """xs, ys: one or two tensors [n_heads, n_tokens, head_dim] of any strides (or Heads), e.g. q and k; ys may be xs.  rope None: the norm alone; else positions as
+    for bs_rope_apply.  Enqueues only."""
+    n, n_tokens, head_dim = len(xs), int(n_tokens), int(head_dim)
+    if len(ys) != n:
+        raise ValueError("as many ys as xs")
+    item, step = _ITEM.get(dtype, 0), n_tokens if axis_stride is None else int(axis_stride)
+    rc = load_library().bs_norm_rope(_norm_ref(norm, head_dim, 0, n - 1), _ref(rope), b"".join([_heads(x, n_tokens, head_dim, item) for x in xs]),
+                                     b"".join([_heads(y, n_tokens, head_dim, item) for y in ys]), n, int(dtype), n_tokens, head_dim,
+                                     None if rope is None else _positions(positions, rope.n_axes, n_tokens, step), step, int(stream) if stream else None)
+    _check(rc, "bs_norm_rope")
+
+
+def bs_norm_rope_grad(norm: Norm, rope: Rope | None, xs, dys, dxs, dweights, dtype: int, n_tokens: int, head_dim: int, positions=None, workspace=None,
+                      axis_stride: int | None = None, stream=None) -> None:
+    """xs, dys, dxs: as xs and ys of bs_norm_rope; dxs may be xs or dys.  dweights: float32 [len(xs), head_dim], contiguous, or None: not wanted, and no workspace is
+    needed then; workspace: a tensor, or (address, bytes), of bs_norm_rope_grad_workspace bytes.  Enqueues only."""
+    n, n_tokens, head_dim = len(xs), int(n_tokens), int(head_dim)
+    if len(dys) != n or len(dxs) != n:
+        raise ValueError("as many dys and dxs as xs")
+    item, step = _ITEM.get(dtype, 0), n_tokens if axis_stride is None else int(axis_stride)
+    rows = [b"".join([_heads(x, n_tokens, head_dim, item) for x in group]) for group in (xs, dys, dxs)]
+    rc = load_library().bs_norm_rope_grad(_norm_ref(norm, head_dim, 0, n - 1), _ref(rope), *rows, _floats(dweights, n * head_dim, "dweights"), n, int(dtype), n_tokens,
+                                          head_dim, None if rope is None else _positions(positions, rope.n_axes, n_tokens, step), step,
+                                          *((None, 0) if workspace is None else _buffer(workspace)), int(stream) if stream else None)
+    _check(rc, "bs_norm_rope_grad")
+
+
+def _floats(x, n: int, name: str):
+    """Address of at least n numbers of float32, one behind the other (a tensor, an address, or None)."""
+    try:
+        fits = x.element_size() == 4 and x.is_floating_point() and x.numel() >= n and x.is_contiguous()
+    except AttributeError:
+        return None if x is None else int(x)
+    if not fits:
+        raise ValueError(f"{name} has to be contiguous float32, {n} numbers")
+    return x.data_ptr()
+
+
+def bs_norm_rope_grad_workspace(n_tensors: int, dtype: int, n_tokens: int, head_dim: int) -> int:
+    n = load_library().bs_norm_rope_grad_workspace(int(n_tensors), int(dtype), int(n_tokens), int(head_dim))
+    if n < 0:
+        _check(int(n), "bs_norm_rope_grad_workspace")
+    return int(n)
+
+
+def bs_cache_append_norm(cache: KVCache, k, v, n_tokens: int, token_seq, token_slot, norm: Norm, rope: Rope | None = None, positions=None,
+                         axis_stride: int | None = None, q=None, q_out=None, slots: CacheSlots | None = None, token_order=None, stream=None) -> None:
+    """bs_cache_append with K normed by the second of norm's weights and q by the first; rope may be None with q, too.  Enqueues only."""
+    n_tokens = int(n_tokens)
+    d, item, step = cache.head_dim, _ITEM.get(cache.dtype, 0), n_tokens if axis_stride is None else int(axis_stride)
+    rc = load_library().bs_cache_append_norm(ctypes.byref(cache), _heads(k, n_tokens, d, item), _heads(v, n_tokens, d, item), n_tokens,
+                                             None if token_seq is None else _ints(token_seq, n_tokens, "token_seq"), _ints(token_slot, n_tokens, "token_slot"),
+                                             _norm_ref(norm, d, 1 if q is None else 0, 1), _ref(rope),
+                                             None if rope is None else _positions(positions, rope.n_axes, n_tokens, step), step,
+                                             None if q is None else _heads(q, n_tokens, d, item), None if q_out is None else _heads(q_out, n_tokens, d, item),
+                                             _slots_ref(slots, cache), None if token_order is None else _ints(token_order, n_tokens, "token_order"),
+                                             int(stream) if stream else None)
+    _check(rc, "bs_cache_append_norm")
+
+
+def _mask(x, n_tokens: int):
+    """Address and words of a mask: a contiguous tensor of 64-bit whole numbers [n_tokens, words], a pair of the two, or None."""
+    if x is None:
+        return None, 0
+    if not hasattr(x, "data_ptr"):
+        address, words = x
+        return int(address), int(words)
+    if x.element_size() != 8 or x.is_floating_point() or x.is_complex() or x.dim() != 2 or x.shape[0] < n_tokens or not x.is_contiguous():
+        raise ValueError(f"mask has to be contiguous int64 [{n_tokens}, words]")
+    return x.data_ptr(), x.shape[1]
+
+
+def bs_attn_tree(cache: KVCache, q, out, n_tokens: int, first, lens, max_tokens: int, scale: float, workspace, mask=None, window: int = 0, cap: float = 0.0,
+                 stream=None) -> None:
+    """q, out: tensors [n_q_heads, n_tokens, head_dim] of any strides (or Heads); first: int32 [n_seqs + 1], lens: int32 [n_seqs] on the device; mask: int64
+    [n_tokens, words] on the device, bit a of a row: it sees drafted token a (None: a chain); workspace: a tensor, or (address, bytes), of
+    bs_attn_tree_workspace bytes.  Enqueues only."""
+    n_tokens = int(n_tokens)
+    n_seqs, d, item = cache.n_seqs, cache.head_dim, _ITEM.get(cache.dtype, 0)
+    rc = load_library().bs_attn_tree(ctypes.byref(cache), _heads(q, n_tokens, d, item), _heads(out, n_tokens, d, item), n_tokens, _ints(first, n_seqs + 1, "first"),
+                                     _ints(lens, n_seqs, "lens"), int(max_tokens), *_mask(mask, n_tokens), int(window), float(scale), float(cap), *_buffer(workspace),
+                                     int(stream) if stream else None)
+    _check(rc, "bs_attn_tree")
+
+
+def bs_attn_tree_workspace(cache: KVCache, n_q_heads: int, n_tokens: int, max_tokens: int) -> int:
+    n = load_library().bs_attn_tree_workspace(ctypes.byref(cache), int(n_q_heads), int(n_tokens), int(max_tokens))
+    if n < 0:
+        _check(int(n), "bs_attn_tree_workspace")
+    return int(n)
+
+
+def bs_cache_accept(cache: KVCache, lens, lens_out, path, n_path, max_path: int | None = None, slots: CacheSlots | None = None, stream=None) -> None:
+    """lens, lens_out, n_path: int32 [n_seqs], path: int32 [n_seqs, max_path] (contiguous; of a tensor max_path is its second size), all on the device; lens and
+    lens_out may be the same.  Enqueues only."""
+    n_seqs = cache.n_seqs
+    if max_path is None:
+        max_path = path.shape[1]
+    elif hasattr(path, "shape") and (path.dim() != 2 or path.shape[1] != max_path):
+        raise ValueError("path has to be [n_seqs, max_path]")
+    rc = load_library().bs_cache_accept(ctypes.byref(cache), _ints(lens, n_seqs, "lens"), _ints(lens_out, n_seqs, "lens_out"), _ints(path, n_seqs * int(max_path), "path"),
+                                        _ints(n_path, n_seqs, "n_path"), int(max_path), _slots_ref(slots, cache), int(stream) if stream else None)
+    _check(rc, "bs_cache_accept")

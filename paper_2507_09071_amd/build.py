@@ -9,7 +9,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libblindsight.so")
-SOURCES = ["tilemap.cpp", "device_map.hip", "attn_prefill.hip", "attn_rows.hip", "attn_f32.hip", "characterize.hip", "rope.hip", "attn_decode.hip", "cache_evict.hip"]
+SOURCES = ["tilemap.cpp", "device_map.hip", "attn_prefill.hip", "attn_rows.hip", "attn_f32.hip", "characterize.hip", "rope.hip", "attn_decode.hip", "cache_evict.hip",
+           "norm_rope.hip", "attn_tree.hip", "cache_accept.hip"]
 
 
 def hipcc() -> str:

@@ -1,0 +1,925 @@
+// Attention of a few drafted tokens per sequence (a tree or a chain) over a paged cache.
+//
+// K and V of a KV head are read once for the T tokens times G query heads that share them, so the work per byte grows with the tree: of a slot's 4 d bytes (bf16)
+// 4 d T G FLOP are made.  Up to about a hundred rows HBM bounds it, beyond that the matrix pipe; fp32 is bounded by the matrix pipe from a few dozen rows on.  How:
+//  * the T G rows of a sequence and KV head are cut into groups of at most M rows; an item is such a group.  M follows from max_tokens G: 16, 32 (four waves that each
+//    take every fourth block of 32 slots, on their own), 64, 128, 256 (eight waves: 2, 4, 8 of them share a block and have 32 rows each, in step).  More rows than
+//    M walk the cache again;
+//  * the blocks of all items lie in one row that is cut into equal shares, one per workgroup, found on the device from the lengths; parts of items that were cut
+//    are joined by a second kernel in a fixed order;
+//  * masks cost nothing but at the end: slots below the length are seen by all, and only blocks that reach behind it (or hold the begin of a window, or a slot
+//    without a page) are masked, by 32 bits per row and block from a copy of the rows' masks in LDS.  A window is laid on the mask when it is copied.
+#include "attn_common.h"
+#include "cache_attn.h"
+
+#include <algorithm>
+#include <cmath>
+#include <mutex>
+#include <type_traits>
+
+#include "device_map.h"
+#include "paged_cache.h"
+
+namespace bs {
+namespace {
+
+// An item in more than one share: the first and the last workgroup that have a part of it.  Filed under the item where there are fewer items than shares
+// (first = last: a whole one), else under the first share (item -1: none goes on behind it).
+struct Cut { int32_t seq, item, first, last; };
+
+struct TreeArgs {
+    bs_cache cache;
+    const void *q;
+    void *out;
+    int64_t q_head, q_token, out_head, out_token;
+    const int32_t *first, *lens;
+    const uint64_t *mask;
+    int32_t n_tokens, max_tokens, mask_words;
+    int32_t G, window, most_items;   // heads per KV head; items of a sequence at most
+    float scale_log2e;            // of scores as they are, or
+    float to_cap, cap_log2e;      // cap > 0: scale / cap, cap log2(e)
+    float *part_o;                // [2 shares][M][d]: of share w, 2 w the item that began before it, 2 w + 1 the one that goes on behind it
+    float2 *part_ml;              // reference point and sum
+    Cut *cuts;
+    int32_t by_item;
+};
+
+// NRB blocks of 16 rows per wave, WR waves that share a block of slots, WK such groups of waves that take turns.
+template <typename T, int D, int NRB, int WR, int WK>
+struct Layout {
+    static constexpr int kWaves = WR * WK, kThreads = 64 * kWaves, kRows = 16 * NRB * WR;
+    static constexpr int kKeys = sizeof(T) == 2 ? 32 : 16;    // slots of a block
+    static constexpr int kRowBytes = D * (int)sizeof(T);
+    static constexpr int kBlock = kKeys * kRowBytes;          // one block of K or V
+    static constexpr int kLoads = kBlock / 1024;              // LDS-direct instructions per block
+    static constexpr int kLoads16 = 16 * kRowBytes / 1024;    // ... per 16 slots, which lie in one page
+    static constexpr int kOwn = (kLoads + WR - 1) / WR;       // ... of a wave
+    static constexpr int kStages = WR > 1 && WK <= 2 && sizeof(T) == 2 ? 3 : 2;
+    static constexpr int kGroup = kStages * 2 * kBlock;       // ring of a group of waves
+    static constexpr int kQuery = WK * kGroup;                // the query rows behind the rings
+    static constexpr int kMerge = WR > 1 ? kRows * D * 4 : kGroup;   // a group's results lie over the ring; where its waves have it alone, over its own part
+    static constexpr int kEnd = kQuery + kRows * kRowBytes > WK * kMerge ? kQuery + kRows * kRowBytes : WK * kMerge;
+    static constexpr int kMask = kEnd;                        // [8][rows]: bits of the drafted tokens
+    static constexpr int kBegin = kMask + 8 * kRows * 4;      // [rows]: first slot seen
+    static constexpr int kMl = kBegin + kRows * 4;            // [groups][rows]
+    static constexpr int kLds = kMl + WK * kRows * 8;
+    static constexpr int kPerCu = D == 64 && WR == 1 ? 2 : 1; // workgroups per CU
+    static_assert((kLds + 1024) * kPerCu <= 160 * 1024, "LDS of a CU");   // (with what own_range has)
+    static_assert(kRows * D * 4 <= kMerge, "a group's results");
+    // exchange of the 16-byte chunks of row r: rows that share their banks get different chunks
+    __device__ static int swizzle(int r) { return kRowBytes == 128 ? (r >> 1) & 7 : r & 15; }
+};
+
+// Beginning an item costs about as much as so many blocks: shares are equal with that counted.
+constexpr int kItemBlocks = 4;
+
+// A sequence: slots in use, its drafted tokens; what is visible of it, from block `first` on; units: of an item, with its beginning; items of it.
+struct Seq { int base, token, T, n, begin, first, blocks, units, groups, items; };
+
+template <int KEYS, int M, typename LOAD>
+__device__ inline Seq seq_of(const TreeArgs &a, int s, LOAD load)
+{
+    Seq v;
+    const int cap = a.cache.max_pages * a.cache.page_size;
+    v.base = max(0, min(load(a.lens + s), cap));
+    v.token = max(0, min(load(a.first + s), a.n_tokens));
+    v.T = min(max(v.token, min(load(a.first + s + 1), a.n_tokens)) - v.token, a.max_tokens);
+    v.n = min(v.base + v.T, cap);
+    v.begin = a.window > 0 ? max(0, v.base - a.window) : 0;
+    v.first = v.begin / KEYS;
+    v.blocks = (v.n + KEYS - 1) / KEYS - v.first;
+    v.groups = (v.T * a.G + M - 1) / M;
+    v.items = v.groups * a.cache.n_kv_heads;
+    v.units = v.T > 0 ? v.blocks + kItemBlocks : 0;
+    return v;
+}
+struct ScalarLoad { __device__ int operator()(const int32_t *p) const { return scalar_load<int>(p); } };
+struct VectorLoad { __device__ int operator()(const int32_t *p) const { return *p; } };
+
+// The share of this workgroup in the row of all units: items of a sequence one behind the other, sequences one behind the other.
+struct Place { int seq, item, unit; };   // sequence, item of it, unit of that
+struct Range { int begin, end; Place at; int each; };   // `each`: units of a share
+
+// All threads of the workgroup; units of a share: a multiple of the groups of waves.
+template <int KEYS, int M, int WK, int THREADS>
+__device__ inline Range own_range(const TreeArgs &a, int share, int n_shares)
+{
+    constexpr int kWaves = THREADS / 64;
+    __shared__ int wave_sums[kWaves], found[3];
+    const int tid = threadIdx.x, S = a.cache.n_seqs;
+    Range r;
+    int total;
+    if (S == 1) {
+        const Seq v = seq_of<KEYS, M>(a, 0, ScalarLoad{});
+        total = v.units * v.items;
+        r.each = max(WK, ((total + n_shares - 1) / n_shares + WK - 1) / WK * WK);
+        r.begin = (int)min((int64_t)total, (int64_t)share * r.each);
+        r.end = min(total, r.begin + r.each);
+        r.at.seq = 0;
+        r.at.item = v.units > 0 ? r.begin / v.units : 0;
+        r.at.unit = r.begin - r.at.item * v.units;
+        return r;
+    }
+    // a thread adds up a few sequences one behind the other
+    const int each = (S + THREADS - 1) / THREADS, s0 = min(S, tid * each), s1 = min(S, s0 + each);
+    int mine = 0;
+    for (int s = s0; s < s1; ++s) {
+        const Seq v = seq_of<KEYS, M>(a, s, VectorLoad{});
+        mine += v.units * v.items;
+    }
+    int upto = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int x = __shfl_up(upto, off, 64);
+        if ((tid & 63) >= off) upto += x;
+    }
+    if ((tid & 63) == 63) wave_sums[tid >> 6] = upto;
+    __syncthreads();
+    total = 0;
+    int before = upto - mine;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        before += w < (tid >> 6) ? wave_sums[w] : 0;
+        total += wave_sums[w];
+    }
+    r.each = max(WK, ((total + n_shares - 1) / n_shares + WK - 1) / WK * WK);
+    r.begin = (int)min((int64_t)total, (int64_t)share * r.each);
+    r.end = min(total, r.begin + r.each);
+    if (r.begin >= before && r.begin < before + mine) {
+        int left = r.begin - before, s = s0;
+        Seq v = seq_of<KEYS, M>(a, s, VectorLoad{});
+        while (left >= v.units * v.items) {
+            left -= v.units * v.items;
+            v = seq_of<KEYS, M>(a, ++s, VectorLoad{});
+        }
+        found[0] = s;
+        found[1] = left / v.units;
+        found[2] = left - left / v.units * v.units;
+    }
+    __syncthreads();
+    r.begin = __builtin_amdgcn_readfirstlane(r.begin);
+    r.end = __builtin_amdgcn_readfirstlane(r.end);
+    r.each = __builtin_amdgcn_readfirstlane(r.each);
+    if (r.begin < r.end) {
+        r.at.seq = __builtin_amdgcn_readfirstlane(found[0]);
+        r.at.item = __builtin_amdgcn_readfirstlane(found[1]);
+        r.at.unit = __builtin_amdgcn_readfirstlane(found[2]);
+    }
+    return r;
+}
+
+// cap tanh(x scale / cap) log2(e).  Below 1 the quotient that the continued fraction of tanh gives after six terms (relative error 3e-9), from there on (e - 1) / (e + 1)
+// with e = exp(2 x): neither loses anything to a difference of numbers that are alike.  (Beyond 15 tanh is 1 to the last bit.)
+__device__ inline float capped(const TreeArgs &a, float s)
+{
+    float x = s * a.to_cap;
+    x = x > 15.f ? 15.f : x;
+    x = x < -15.f ? -15.f : x;   // (a NaN stays one)
+    const float x2 = x * x, e = __builtin_amdgcn_exp2f(x * 2.8853900817779268f);
+    const bool small = x2 < 1.f;
+    const float num = small ? x * fmaf(x2, fmaf(x2, 21.f, 1260.f), 10395.f) : e - 1.f;
+    const float den = small ? fmaf(x2, fmaf(x2, x2 + 210.f, 4725.f), 10395.f) : e + 1.f;
+    return num * __builtin_amdgcn_rcpf(den) * a.cap_log2e;
+}
+
+template <typename T, int D, int NRB, int WR, int WK>
+__global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * WR * WK + 3) / 4) void tree_shares(const TreeArgs a)
+{
+    using TR = Layout<T, D, NRB, WR, WK>;
+    constexpr bool BF16 = sizeof(T) == 2, SHARED = WR > 1;
+    constexpr int KEYS = TR::kKeys, ROWB = TR::kRowBytes, BLK = TR::kBlock, NI = TR::kLoads, NI16 = TR::kLoads16, SUB = KEYS / 16, OWN = TR::kOwn;
+    constexpr int ROWS = TR::kRows, NB = D / 16, CH4 = D / 4, WAVES = TR::kWaves, THREADS = TR::kThreads, STAGES = TR::kStages, KSTEPS = D * (int)sizeof(T) / 64;
+    extern __shared__ __align__(1024) unsigned char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wk = wave / WR, wr = wave % WR;
+    const int P = a.cache.page_size, cap = a.cache.max_pages * P;
+
+    // items that a sequence could have and has not: nothing to join
+    if (a.by_item)
+        for (int s = blockIdx.x; s < a.cache.n_seqs; s += gridDim.x)
+            for (int i = seq_of<KEYS, ROWS>(a, s, ScalarLoad{}).items + tid; i < a.most_items; i += THREADS) a.cuts[s * a.most_items + i] = Cut{s, i, 0, 0};
+
+    const Range range = own_range<KEYS, ROWS, WK, THREADS>(a, blockIdx.x, gridDim.x);
+    if (tid == 0 && !a.by_item) a.cuts[blockIdx.x] = Cut{0, -1, 0, 0};
+    if (range.begin >= range.end) return;
+
+    typedef __attribute__((address_space(3))) void *lds_ptr;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr)lds, ring = lds0 + wk * TR::kGroup;
+    // LDS-direct loads: instruction j of 16 slots moves 1 KB, i.e. 1024 / ROWB whole rows; a lane picks the chunk of its row that belongs at
+    // its place.  The waves that share a block take every WR-th of its instructions.
+    uint32_t voff[OWN];
+#pragma unroll
+    for (int x = 0; x < OWN; ++x) {
+        const int j = (x * WR + wr) % NI16, r = j * (1024 / ROWB) + lane / (ROWB / 16), p = lane % (ROWB / 16);
+        voff[x] = r * (uint32_t)(a.cache.slot_stride * sizeof(T)) + ((p ^ TR::swizzle(r)) << 4);
+    }
+    const auto load_lds = [](uint32_t off, const char *src, uint32_t dst) __attribute__((always_inline)) {
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(src), "s"(dst) : "memory", "m0");
+    };
+    const auto wait_loads = [](auto newer) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(newer)::value) : "memory");
+    };
+    const auto reads_done = []() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+    const auto meet = []() __attribute__((always_inline)) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    const uint32_t k_read = wk * TR::kGroup + col * ROWB + ((grp ^ TR::swizzle(col)) << 4);
+    uint32_t v_read[BF16 ? 2 : 4];   // bf16: of the two halves of a block; fp32: of the four slots of a lane
+    if constexpr (BF16) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = 16 * h + 4 * grp + (col >> 2);
+            v_read[h] = wk * TR::kGroup + BLK + r * ROWB + ((((col >> 1) & 1) ^ TR::swizzle(r)) << 4) + (col & 1) * 8;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 4 * grp + i;
+            v_read[i] = wk * TR::kGroup + BLK + r * ROWB + ((col ^ TR::swizzle(r)) << 4);
+        }
+    }
+    const uint32_t *row_mask = reinterpret_cast<const uint32_t *>(lds + TR::kMask);
+    const int *row_begin = reinterpret_cast<const int *>(lds + TR::kBegin);
+
+    Place at = range.at;
+    int pos = range.begin;
+    Seq seq = seq_of<KEYS, ROWS>(a, at.seq, ScalarLoad{});
+    while (pos < range.end) {
+        while (at.item == seq.items) {   // the next sequence that has some
+            at.item = 0;
+            seq = seq_of<KEYS, ROWS>(a, ++at.seq, ScalarLoad{});
+        }
+        const int block = max(0, at.unit - kItemBlocks);   // the first one
+        const int blocks = min(seq.blocks - block, range.end - pos - max(0, kItemBlocks - at.unit));
+        if (blocks <= 0) break;   // the share ends where the item begins
+        const int kvh = at.item / seq.groups, row0 = (at.item - kvh * seq.groups) * ROWS;   // rows: token by token, the group's heads of each
+        const int n_rows = min(ROWS, seq.T * a.G - row0);
+        // Waves that share their blocks step together, and one group may have none in the last step.
+        const int n_steps = SHARED ? (blocks + WK - 1) / WK : (blocks > wk ? (blocks - wk + WK - 1) / WK : 0);
+        const int b0 = seq.first + block + wk;   // step i: block b0 + WK i of the sequence
+
+        // Page numbers of 16 slots each; which slots of a block have a page.
+        const int32_t *table = a.cache.page_table + (int64_t)at.seq * a.cache.max_pages;
+        struct Pages { int32_t page[SUB]; uint32_t in_page[SUB]; };
+        const auto pages_of = [&](int i) __attribute__((always_inline)) {
+            Pages p;
+#pragma unroll
+            for (int h = 0; h < SUB; ++h) {
+                // (behind the last slots: those again)
+                const uint32_t slot = min((b0 + WK * min(i, n_steps - 1)) * KEYS + 16 * h, cap - 16);
+                const uint32_t page = slot / (uint32_t)P;
+                p.page[h] = scalar_load<int>(table + page);
+                p.in_page[h] = slot - page * P;
+            }
+            return p;
+        };
+        struct Sources { const char *k[SUB], *v[SUB]; uint32_t there; };
+        const auto sources_of = [&](const Pages &p) __attribute__((always_inline)) {
+            Sources s;
+            s.there = 0;
+#pragma unroll
+            for (int h = 0; h < SUB; ++h) {
+                const bool ok = (uint32_t)p.page[h] < (uint32_t)a.cache.n_pages;
+                const int64_t off = ((ok ? p.page[h] : 0) * a.cache.page_stride + kvh * a.cache.head_stride + p.in_page[h] * a.cache.slot_stride) * (int64_t)sizeof(T);
+                s.k[h] = static_cast<const char *>(a.cache.k) + off;
+                s.v[h] = static_cast<const char *>(a.cache.v) + off;
+                s.there |= ok ? 0xffffu << (16 * h) : 0u;
+            }
+            return s;
+        };
+        const auto issue = [&](const char *const(&src)[SUB], uint32_t dst) __attribute__((always_inline)) {
+#pragma unroll
+            for (int x = 0; x < OWN; ++x) {
+                const int j = x * WR + wr;
+                if (NI % WR == 0 || j < NI) load_lds(voff[x], src[SUB == 1 || j < NI16 ? 0 : SUB - 1], dst + j * 1024);
+            }
+        };
+
+        // The query rows (all waves together) in the layout of a K block, then the first blocks of keys and values.  A place without a row holds a copy of the last
+        // one, whose results are not stored.
+        {
+            const char *qh = reinterpret_cast<const char *>(static_cast<const T *>(a.q) + seq.token * a.q_token + (int64_t)kvh * a.G * a.q_head);
+            constexpr int kAll = ROWS * ROWB / 1024;
+#pragma unroll
+            for (int i0 = 0; i0 < kAll; i0 += WAVES) {
+                const int i = i0 + wave;
+                if (kAll % WAVES == 0 || i < kAll) {
+                    const int r = i * (1024 / ROWB) + lane / (ROWB / 16), p = lane % (ROWB / 16);
+                    const int R = row0 + min(r, n_rows - 1), t = R / a.G;
+                    load_lds((uint32_t)((t * a.q_token + (R - t * a.G) * a.q_head) * (int64_t)sizeof(T)) + ((p ^ TR::swizzle(r)) << 4), qh, lds0 + TR::kQuery + i * 1024);
+                }
+            }
+        }
+        Sources s0{}, s1{};
+        Pages next{};
+        if (n_steps > 0) {
+            const Pages p0 = pages_of(0), p1 = pages_of(1);
+            next = pages_of(2);
+            s0 = sources_of(p0);
+            issue(s0.k, ring);
+            issue(s0.v, ring + BLK);
+            s1 = sources_of(p1);
+            if (n_steps > 1 && (!SHARED || STAGES > 2)) {
+                issue(s1.k, ring + 2 * BLK);
+                issue(s1.v, ring + 3 * BLK);
+            }
+        }
+        // What the rows see of the drafted tokens, and where a window begins
+        for (int r = tid; r < ROWS; r += THREADS) {
+            const int t = (row0 + min(r, n_rows - 1)) / a.G;
+            uint64_t words[BS_TREE_MAX_TOKENS / 64];
+            int seen = 0;
+#pragma unroll
+            for (int w = 0; w < BS_TREE_MAX_TOKENS / 64; ++w) {
+                uint64_t x = a.mask ? 0 : bits_between(0, t + 1 - 64 * w);
+                if (a.mask && w < a.mask_words) x = a.mask[(int64_t)(seq.token + t) * a.mask_words + w];
+                words[w] = x & bits_between(0, seq.T - 64 * w);
+                seen += __popcll(words[w]);
+            }
+            int begin = 0;
+            if (a.window > 0) {
+                begin = max(0, seq.base - max(0, a.window - seen));
+                int drop = seen - a.window;   // the first ones
+#pragma unroll
+                for (int w = 0; w < BS_TREE_MAX_TOKENS / 64; ++w) {
+                    const int n = __popcll(words[w]);
+                    if (drop >= n) words[w] = 0;
+                    else for (int i = 0; i < drop; ++i) words[w] &= words[w] - 1;
+                    drop -= n;
+                }
+            }
+#pragma unroll
+            for (int w = 0; w < 8; ++w) reinterpret_cast<uint32_t *>(lds + TR::kMask)[w * ROWS + r] = (uint32_t)(words[w / 2] >> (32 * (w % 2)));
+            reinterpret_cast<int *>(lds + TR::kBegin)[r] = begin;
+        }
+        if (!SHARED && n_steps > 1) wait_loads(std::integral_constant<int, 4 * NI>{});
+        else if (!SHARED && n_steps == 1) wait_loads(std::integral_constant<int, 2 * NI>{});
+        else wait_loads(std::integral_constant<int, 0>{});
+        reads_done();
+        meet();
+        uint4 q[NRB][KSTEPS];
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+            for (int t = 0; t < KSTEPS; ++t)
+                q[rb][t] = *reinterpret_cast<const uint4 *>(lds + TR::kQuery + (wr * NRB + rb) * 16 * ROWB + ((col * ROWB + ((grp ^ TR::swizzle(col)) << 4)) ^ (t << 6)));
+
+        floatx4 o[NRB][NB];
+        float m_run[NRB], l_run[NRB];
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+            m_run[rb] = -INFINITY;
+            l_run[rb] = 0.f;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[rb][nb][i] = 0.f;
+        }
+        const float c = a.cap_log2e > 0.f ? 1.f : a.scale_log2e;   // of scores that are not capped
+        // Slots below this one, if their pages are there, are seen by all rows, but for those before the window's last begin.
+        const int window_end = a.window > 0 ? min(seq.base, seq.base - a.window + seq.T) : 0;
+
+        uint32_t there0 = s0.there, there1 = s1.there;   // of this block, of the next one
+        int stage = 0;                                   // offset of this block's stage
+        for (int i = 0; i < n_steps; ++i) {
+            const bool more = i + 1 < n_steps, more2 = i + 2 < n_steps;
+            const int n0 = (b0 + WK * i) * KEYS;
+            Sources s2{};
+            if (SHARED) {
+                if (STAGES > 2 && more) wait_loads(std::integral_constant<int, 2 * OWN>{});
+                else wait_loads(std::integral_constant<int, 0>{});
+                meet();   // all of the block is there, and the stage of the block before is free
+                if constexpr (STAGES > 2) {
+                    if (more2) {
+                        s2 = sources_of(next);
+                        const int to = stage == 0 ? 4 * BLK : stage - 2 * BLK;
+                        issue(s2.k, ring + to);
+                        issue(s2.v, ring + to + BLK);
+                    }
+                } else {
+                    if (more) {
+                        issue(s1.k, ring + (stage ^ 2 * BLK));
+                        issue(s1.v, ring + (stage ^ 2 * BLK) + BLK);
+                    }
+                    if (more2) s1 = s2 = sources_of(next);
+                }
+            } else if (more2) {
+                s2 = sources_of(next);
+            }
+            next = pages_of(i + 3);
+
+            // ---- S^T = K Q^T: lane: slots 16 h + 4 grp + e of query row `col` of each row block
+            if constexpr (!SHARED) {
+                if (!more) wait_loads(std::integral_constant<int, NI>{});
+                else wait_loads(std::integral_constant<int, 3 * NI>{});
+            }
+            floatx4 s[NRB][SUB];
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+                for (int h = 0; h < SUB; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[rb][h][e] = 0.f;
+#pragma unroll
+            for (int t = 0; t < KSTEPS; ++t)
+#pragma unroll
+                for (int h = 0; h < SUB; ++h) {
+                    const uint4 f = *reinterpret_cast<const uint4 *>(lds + ((k_read + stage) ^ (t << 6)) + h * 16 * ROWB);
+#pragma unroll
+                    for (int rb = 0; rb < NRB; ++rb) {
+                        if constexpr (BF16) {
+                            s[rb][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, q[rb][t]), s[rb][h], 0, 0, 0);
+                        } else {
+                            const floatx4 x = __builtin_bit_cast(floatx4, f), y = __builtin_bit_cast(floatx4, q[rb][t]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[rb][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], s[rb][h], 0, 0, 0);
+                        }
+                    }
+                }
+            if constexpr (!SHARED) {
+                reads_done();
+                if (more2) issue(s2.k, ring + stage);
+            }
+            if (a.cap_log2e > 0.f) {
+#pragma unroll
+                for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+                    for (int h = 0; h < SUB; ++h)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[rb][h][e] = capped(a, s[rb][h][e]);
+            }
+
+            // ---- which of the lane's slots its rows see (4 bits per 16 slots)
+            uint32_t exists = there0;   // slots that may be looked at
+            if (n0 < seq.begin) exists &= ~0u << min(31, seq.begin - n0);   // (a block has a visible slot: seq.begin - n0 < KEYS)
+            if (n0 + KEYS > seq.n) exists &= n0 < seq.n ? ~(~0u << (seq.n - n0)) : 0u;
+            if (SHARED && block + wk + WK * i >= block + blocks) exists = 0;   // the group has no block in this step
+            const bool masked = n0 + KEYS > seq.base || n0 < window_end || exists != (KEYS == 32 ? ~0u : 0xffffu);
+            uint32_t seen[NRB];
+            if (masked) {
+#pragma unroll
+                for (int rb = 0; rb < NRB; ++rb) {
+                    const int row = (wr * NRB + rb) * 16 + col, rel = n0 - seq.base;   // drafted token of the first slot
+                    uint32_t x;
+                    if (rel >= 0) {
+                        const int w = min(rel >> 5, 8);
+                        const uint32_t lo = w < 8 ? row_mask[w * ROWS + row] : 0, hi = w < 7 ? row_mask[(w + 1) * ROWS + row] : 0;
+                        x = __builtin_amdgcn_alignbit(hi, lo, rel & 31);
+                    } else {
+                        x = rel > -32 ? (row_mask[row] << (-rel & 31)) | ~(~0u << (-rel & 31)) : ~0u;
+                    }
+                    const int before = row_begin[row] - n0;   // slots that lie before the row's window
+                    if (before > 0) x &= before < 32 ? ~0u << before : 0u;
+                    seen[rb] = (x & exists) >> (4 * grp);
+#pragma unroll
+                    for (int h = 0; h < SUB; ++h)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[rb][h][e] = (seen[rb] & (1u << (16 * h + e))) ? s[rb][h][e] : -INFINITY;
+                }
+            }
+
+            // ---- the running maximum and sum
+            float p[NRB][SUB][4];
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int h = 0; h < SUB; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[rb][h][e]);
+                mx = max_across_groups(mx);
+                // the reference point moves only when the block's maximum exceeds it by 2^8 (any reference gives the same quotient),
+                // so the accumulators are rescaled a few times per row and not once per block
+                const bool grow = fmaf(mx, c, -(m_run[rb] * c)) > 8.f;
+                const float m_new = grow ? mx : m_run[rb];
+                const float off = m_new == -INFINITY ? 0.f : -(m_new * c);   // no slot so far: p = 0
+                const float alpha = grow ? __builtin_amdgcn_exp2f(fmaf(m_run[rb], c, off)) : 1.f;
+                float sum = 0.f;
+#pragma unroll
+                for (int h = 0; h < SUB; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p[rb][h][e] = __builtin_amdgcn_exp2f(fmaf(s[rb][h][e], c, off));
+                        sum += p[rb][h][e];
+                    }
+                l_run[rb] = fmaf(l_run[rb], alpha, sum);
+                m_run[rb] = m_new;
+                if (__any(alpha != 1.f)) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[rb][nb][e] *= alpha;
+                }
+            }
+
+            // ---- O^T += V^T P^T
+            if constexpr (!SHARED) {
+                if (more2) wait_loads(std::integral_constant<int, 3 * NI>{});
+                else if (more) wait_loads(std::integral_constant<int, 2 * NI>{});
+                else wait_loads(std::integral_constant<int, 0>{});
+            }
+            typedef __attribute__((address_space(3))) bf16x4 *lds_bf16x4;
+            const auto read_v = [&](int nb) __attribute__((always_inline)) {   // bf16: channel 16 nb + col, slots 4 grp .. + 3 of both halves
+                uint4 f;
+                const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(lds + ((v_read[0] + stage) ^ (nb << 5)))));
+                const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(lds + ((v_read[BF16 ? 1 : 0] + stage) ^ (nb << 5)))));
+                f.x = x.x; f.y = x.y; f.z = y.x; f.w = y.y;
+                return f;
+            };
+            // Values that no row of the call may look at, and any infinity or NaN in a masked block, are replaced by zero: times a probability of zero they would be
+            // a NaN.  Rows that do see such a value get one through their sum.
+            const uint32_t mine = exists >> (4 * grp);
+            uint32_t bad = 0;   // of the lane's slots: a value that is not finite
+            if (masked) {
+                uint32_t most[4] = {0, 0, 0, 0};   // bf16: two slots in each; fp32: one
+                if constexpr (BF16) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        const uint4 f = read_v(nb);
+                        const uint32_t x[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            if ((x[w] & 0x7f80u) == 0x7f80u) most[w] |= 1u;
+                            if ((x[w] & 0x7f800000u) == 0x7f800000u) most[w] |= 2u;
+                        }
+                    }
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) bad |= most[w] << (16 * (w / 2) + 2 * (w % 2));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int n = 0; n < D / 64; ++n) {
+                            const uint4 f = *reinterpret_cast<const uint4 *>(lds + v_read[BF16 ? 0 : e] + stage + n * 256);
+                            const uint32_t x[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+                            for (int w = 0; w < 4; ++w)
+                                if ((x[w] & 0x7f800000u) == 0x7f800000u) bad |= 1u << e;
+                        }
+                }
+#pragma unroll
+                for (int off = 1; off < 16; off <<= 1) bad |= __shfl_xor(bad, off, 64);   // all channels: the lanes of the same slots
+#pragma unroll
+                for (int rb = 0; rb < NRB; ++rb)
+                    if (seen[rb] & bad) l_run[rb] = __builtin_nanf("");
+            }
+            const uint32_t fine = mine & ~bad;   // (a slot with a value that is not finite: all of its values)
+            if constexpr (BF16) {
+                // Probabilities in two bf16 numbers each, 16 bits of their fraction.  One number would do half the work here, but is as coarse as the result's own
+                // rounding, which then is off by 1.4 times as much.
+                bf16x8 pb[NRB], rest[NRB];
+#pragma unroll
+                for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float x = p[rb][e >> 2][e & 3];
+                        pb[rb][e] = (__bf16)x;
+                        rest[rb][e] = (__bf16)(x - (float)pb[rb][e]);
+                    }
+                uint32_t keep[4];
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int at = 16 * (w / 2) + 2 * (w % 2);
+                    keep[w] = ((fine >> at) & 1 ? 0xffffu : 0u) | ((fine >> (at + 1)) & 1 ? 0xffff0000u : 0u);
+                }
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    uint4 f = read_v(nb);
+                    f.x &= keep[0]; f.y &= keep[1]; f.z &= keep[2]; f.w &= keep[3];
+#pragma unroll
+                    for (int rb = 0; rb < NRB; ++rb) {
+                        o[rb][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), pb[rb], o[rb][nb], 0, 0, 0);
+                        o[rb][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), rest[rb], o[rb][nb], 0, 0, 0);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)   // slot 4 grp + e
+#pragma unroll
+                    for (int n = 0; n < D / 64; ++n) {
+                        floatx4 x = *reinterpret_cast<const floatx4 *>(lds + v_read[BF16 ? 0 : e] + stage + n * 256);
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            x[w] = (fine & (1u << e)) ? x[w] : 0.f;
+#pragma unroll
+                            for (int rb = 0; rb < NRB; ++rb) o[rb][4 * n + w] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[w], p[rb][0][e], o[rb][4 * n + w], 0, 0, 0);
+                        }
+                    }
+            }
+            reads_done();
+            if constexpr (!SHARED) {
+                if (more2) issue(s2.v, ring + stage + BLK);
+            }
+            there0 = there1;
+            there1 = s2.there;
+            stage = stage + 2 * BLK == STAGES * 2 * BLK ? 0 : stage + 2 * BLK;
+        }
+
+        // ---- the groups' results over the rings; [row][chunks of 4 channels, exchanged]
+        if constexpr (SHARED) meet();   // all waves have read their last block
+        float2 *ml = reinterpret_cast<float2 *>(lds + TR::kMl);   // [group][row]
+        float4 *merge = reinterpret_cast<float4 *>(lds);
+        constexpr int kMergeGroup = TR::kMerge / 16;
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+            const int row = (wr * NRB + rb) * 16 + col;
+            const float l = sum_across_groups(l_run[rb]);
+            if (grp == 0) ml[wk * ROWS + row] = make_float2(m_run[rb], l);
+            if (row < n_rows) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    if constexpr (BF16) {   // channels 16 nb + 4 grp + i
+                        merge[wk * kMergeGroup + row * CH4 + ((nb * 4 + grp) ^ (row & (CH4 - 1)))] = make_float4(o[rb][nb][0], o[rb][nb][1], o[rb][nb][2], o[rb][nb][3]);
+                    } else {                // channel 64 n + 16 grp + 4 i + w of o[4 n + w][i]: here nb = 4 n + i
+                        const int n = nb / 4, i = nb % 4;
+                        merge[wk * kMergeGroup + row * CH4 + ((16 * n + 4 * grp + i) ^ (row & (CH4 - 1)))] =
+                            make_float4(o[rb][4 * n][i], o[rb][4 * n + 1][i], o[rb][4 * n + 2][i], o[rb][4 * n + 3][i]);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        const bool begins = block == 0, ends = block + blocks == seq.blocks;
+        const int64_t part = (int64_t)(2 * blockIdx.x + (begins ? 1 : 0)) * ROWS;
+        for (int idx = tid; idx < n_rows * CH4; idx += THREADS) {
+            const int row = idx / CH4, ch = idx % CH4;
+            float2 x[WK];
+            float4 y[WK];
+            float m = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int w = 0; w < WK; ++w) {
+                x[w] = ml[w * ROWS + row];
+                y[w] = merge[w * kMergeGroup + row * CH4 + (ch ^ (row & (CH4 - 1)))];
+                m = fmaxf(m, x[w].x);
+            }
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < WK; ++w) {
+                const float f = x[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[w].x - m) * c);
+                l = fmaf(x[w].y, f, l);
+                sum.x = fmaf(y[w].x, f, sum.x); sum.y = fmaf(y[w].y, f, sum.y); sum.z = fmaf(y[w].z, f, sum.z); sum.w = fmaf(y[w].w, f, sum.w);
+            }
+            if (begins && ends) {
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                const int R = row0 + row, t = R / a.G;
+                store_row4(static_cast<T *>(a.out) + (seq.token + t) * a.out_token + (int64_t)(kvh * a.G + R - t * a.G) * a.out_head + 4 * ch,
+                           make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+            } else {
+                *reinterpret_cast<float4 *>(a.part_o + (part + row) * D + 4 * ch) = sum;
+                if (ch == 0) a.part_ml[part + row] = make_float2(m, l);
+            }
+        }
+        if (begins && tid == 0 && (a.by_item || !ends))
+            a.cuts[a.by_item ? at.seq * a.most_items + at.item : (int)blockIdx.x] = Cut{at.seq, at.item, (int)blockIdx.x, (pos - at.unit + seq.units - 1) / range.each};
+        pos += seq.units - at.unit;   // (behind the share's end if the item is cut)
+        at.unit = 0;
+        ++at.item;
+        if (pos < range.end) __syncthreads();   // the LDS is free again
+    }
+}
+
+// Joins the parts of a row (blockIdx.y) of an item that was cut (blockIdx.x): threads are D / 4 channel quads times the parts side by side, in a
+// fixed order.
+template <typename T, int D, int M>
+__global__ __launch_bounds__(256) void tree_join(const TreeArgs a)
+{
+    constexpr int CH4 = D / 4, LANES = 256 / CH4;
+    __shared__ float4 acc[LANES][CH4];
+    __shared__ float2 ml[LANES];
+    const int tid = threadIdx.x, ch = tid % CH4, p0 = tid / CH4, row = blockIdx.y;
+    const Cut cut = a.cuts[blockIdx.x];
+    if (a.by_item ? cut.first == cut.last : cut.item < 0) return;
+    const Seq seq = seq_of<sizeof(T) == 2 ? 32 : 16, M>(a, cut.seq, VectorLoad{});
+    const int kvh = cut.item / seq.groups, row0 = (cut.item - kvh * seq.groups) * M;
+    if (row >= min(M, seq.T * a.G - row0)) return;
+    const float c = a.cap_log2e > 0.f ? 1.f : a.scale_log2e;
+    float m = -INFINITY, l = 0.f;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    // loads of eight parts go out together ; those behind the last one to that one
+    for (int w0 = cut.first + p0; w0 <= cut.last; w0 += 8 * LANES) {
+        float2 x[8];
+        float4 y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int w = min(w0 + i * LANES, cut.last);
+            const int64_t at = (int64_t)(2 * w + (w == cut.first ? 1 : 0)) * M + row;
+            x[i] = a.part_ml[at];
+            y[i] = *reinterpret_cast<const float4 *>(a.part_o + at * D + 4 * ch);
+        }
+        const float m_old = m;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, x[i].x);
+        const float old = m_old == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_old - m) * c);
+        l *= old;
+        sum.x *= old; sum.y *= old; sum.z *= old; sum.w *= old;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (w0 + i * LANES > cut.last) continue;
+            const float f = x[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[i].x - m) * c);
+            l = fmaf(x[i].y, f, l);
+            sum.x = fmaf(y[i].x, f, sum.x); sum.y = fmaf(y[i].y, f, sum.y); sum.z = fmaf(y[i].z, f, sum.z); sum.w = fmaf(y[i].w, f, sum.w);
+        }
+    }
+    acc[p0][ch] = sum;
+    if (ch == 0) ml[p0] = make_float2(m, l);
+    __syncthreads();
+    if (tid >= CH4) return;
+    m = -INFINITY;
+    l = 0.f;
+    sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < LANES; ++i) m = fmaxf(m, ml[i].x);
+#pragma unroll
+    for (int i = 0; i < LANES; ++i) {
+        const float g = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[i].x - m) * c);
+        const float4 y = acc[i][ch];
+        l = fmaf(ml[i].y, g, l);
+        sum.x = fmaf(y.x, g, sum.x); sum.y = fmaf(y.y, g, sum.y); sum.z = fmaf(y.z, g, sum.z); sum.w = fmaf(y.w, g, sum.w);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int R = row0 + row, t = R / a.G;
+    store_row4(static_cast<T *>(a.out) + (seq.token + t) * a.out_token + (int64_t)(kvh * a.G + R - t * a.G) * a.out_head + 4 * ch,
+               make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+}
+
+// ------------------------------------------------------------------------------------ host
+
+constexpr int kMaxDevices = 64;
+std::mutex g_mutex;
+int g_n_cus[kMaxDevices];   // compute units of a device, once its kernels' limits are raised
+
+// The kernel for up to M rows of a sequence and KV head: f(NRB, WR, WK as types).  fp32: 256 rows of queries would not fit beside the ring, nor would four
+// rings beside 64.
+template <typename T, typename F>
+auto with_rows(int32_t M, F f)
+{
+    using std::integral_constant;
+    typedef integral_constant<int, 1> one;
+    typedef integral_constant<int, 2> two;
+    typedef integral_constant<int, 4> four;
+    typedef integral_constant<int, 8> eight;
+    switch (M) {
+    case 16: return f(one{}, one{}, four{});
+    case 32: return f(two{}, one{}, four{});
+    case 64:
+        if constexpr (sizeof(T) == 2) return f(two{}, two{}, four{});
+        else return f(two{}, two{}, two{});
+    case 128: return f(two{}, four{}, two{});
+    default:
+        if constexpr (sizeof(T) == 2) return f(two{}, eight{}, one{});
+        else return f(two{}, four{}, two{});
+    }
+}
+
+int32_t rows_of(int64_t rows, int32_t dtype)
+{
+    return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 || dtype == BS_F32 ? 128 : 256;
+}
+
+template <typename T, int D>
+hipError_t raise_limits()
+{
+    for (int M : {16, 32, 64, 128, 256}) {
+        const hipError_t e = with_rows<T>(M, [](auto nrb, auto wr, auto wk) {
+            constexpr int NRB = decltype(nrb)::value, WR = decltype(wr)::value, WK = decltype(wk)::value;
+            return hipFuncSetAttribute(reinterpret_cast<const void *>(tree_shares<T, D, NRB, WR, WK>), hipFuncAttributeMaxDynamicSharedMemorySize, Layout<T, D, NRB, WR, WK>::kLds);
+        });
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+int device_setup(int *n_cus)
+{
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return fail_hip(e, "hipGetDevice");
+    if (dev < 0 || dev >= kMaxDevices) return fail_msg(BS_EUNSUPPORTED, "device ordinal above 63");
+    std::lock_guard<std::mutex> lock(g_mutex);
+    if (g_n_cus[dev] == 0) {
+        e = raise_limits<__bf16, 64>();
+        if (e == hipSuccess) e = raise_limits<__bf16, 128>();
+        if (e == hipSuccess) e = raise_limits<float, 64>();
+        if (e == hipSuccess) e = raise_limits<float, 128>();
+        if (e != hipSuccess) return fail_hip(e, "hipFuncSetAttribute");
+        int cus = 0;
+        e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+        if (e != hipSuccess || cus <= 0) return fail_hip(e, "hipDeviceGetAttribute(compute units)");
+        g_n_cus[dev] = cus;
+    }
+    *n_cus = g_n_cus[dev];
+    return BS_OK;
+}
+
+int check_tree(const bs_cache *cache, int32_t n_q_heads, int32_t n_tokens, int32_t max_tokens)
+{
+    if (int rc = check_cache(cache)) return rc;
+    if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads != 0 || n_tokens < 0 || max_tokens < 1 || max_tokens > BS_TREE_MAX_TOKENS) return BS_EINVAL;
+    if (cache->head_dim != 64 && cache->head_dim != 128) return BS_EUNSUPPORTED;
+    return BS_OK;
+}
+
+// How a call is laid out over the chip and its workspace: nothing but sizes, so that a graph of a call stays right when lengths change.
+struct Plan {
+    int32_t M, n_shares, n_cuts, most_items;      // rows of an item; shares; entries of cuts; items of a sequence
+    int64_t part_o, part_ml, cuts, bytes;         // offsets
+};
+
+int make_plan(const bs_cache &c, int32_t n_q_heads, int32_t n_tokens, int32_t max_tokens, int n_cus, Plan *p)
+{
+    const int32_t G = n_q_heads / c.n_kv_heads, keys = c.dtype == BS_BF16 ? 32 : 16;
+    const int64_t rows = (int64_t)G * std::min(std::max(1, n_tokens), max_tokens);   // of a sequence and KV head
+    if (rows > 1 << 24) return BS_EUNSUPPORTED;
+    p->M = rows_of(rows, c.dtype);
+    const int64_t groups = (rows + p->M - 1) / p->M, per_item = (cache_slots(c) + keys - 1) / keys + 1, items = (int64_t)c.n_seqs * c.n_kv_heads;
+    if (items > INT32_MAX / groups || items * groups > INT32_MAX / 2 / (per_item + kItemBlocks)) return BS_EUNSUPPORTED;   // units are counted in 32 bits
+    p->most_items = (int32_t)(groups * c.n_kv_heads);
+    const int per_cu = c.head_dim == 64 && p->M <= 32 ? 2 : 1, turns = p->M <= (c.dtype == BS_BF16 ? 64 : 32) ? 4 : p->M <= 128 ? 2 : 1;   // (see Layout)
+    p->n_shares = (int32_t)std::min<int64_t>((int64_t)n_cus * per_cu, (items * groups * per_item + turns - 1) / turns);
+    const auto whole = [](int64_t bytes) { return (bytes + 255) / 256 * 256; };
+    p->part_o = 0;
+    p->part_ml = whole((int64_t)2 * p->n_shares * p->M * c.head_dim * 4);
+    p->cuts = p->part_ml + whole((int64_t)2 * p->n_shares * p->M * 8);
+    p->n_cuts = (int32_t)std::min<int64_t>(p->n_shares, items * groups);
+    p->bytes = p->cuts + whole((int64_t)p->n_cuts * sizeof(Cut));
+    return BS_OK;
+}
+
+template <typename T, int D>
+int launch(const TreeArgs &a, const Plan &p, hipStream_t st)
+{
+    return with_rows<T>(p.M, [&](auto nrb, auto wr, auto wk) {
+        constexpr int NRB = decltype(nrb)::value, WR = decltype(wr)::value, WK = decltype(wk)::value;
+        using L = Layout<T, D, NRB, WR, WK>;
+        hipError_t e = launch_kernel(tree_shares<T, D, NRB, WR, WK>, dim3((unsigned)p.n_shares), dim3(L::kThreads), L::kLds, st, a);
+        if (e != hipSuccess) return fail_hip(e, "tree_shares launch");
+        if (p.n_shares > 1) e = launch_kernel(tree_join<T, D, L::kRows>, dim3((unsigned)p.n_cuts, (unsigned)L::kRows), dim3(256), 0, st, a);
+        return e == hipSuccess ? BS_OK : fail_hip(e, "tree_join launch");
+    });
+}
+
+}  // namespace
+}  // namespace bs
+
+extern "C" int64_t bs_attn_tree_workspace(const bs_cache *cache, int32_t n_q_heads, int32_t n_tokens, int32_t max_tokens)
+{
+    using namespace bs;
+    if (int rc = check_tree(cache, n_q_heads, n_tokens, max_tokens)) return rc;
+    int n_cus = 0;
+    Plan p;
+    if (int rc = device_setup(&n_cus)) return rc;
+    if (int rc = make_plan(*cache, n_q_heads, n_tokens, max_tokens, n_cus, &p)) return rc;
+    return p.bytes;
+}
+
+extern "C" int bs_attn_tree(const bs_cache *cache, const bs_heads *q, const bs_heads *out, int32_t n_tokens, const int32_t *first, const int32_t *lens, int32_t max_tokens,
+                            const uint64_t *mask, int32_t mask_words, int32_t window, float scale, float cap, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    using namespace bs;
+    const bool none = n_tokens == 0;
+    if (check_heads(q, none) || check_heads(out, none) || q->n_heads != out->n_heads || !first || !lens || window < 0) return BS_EINVAL;
+    if (!(scale > 0.f) || !std::isfinite(scale) || !(cap >= 0.f) || !std::isfinite(cap)) return BS_EINVAL;
+    if (int rc = check_tree(cache, q->n_heads, n_tokens, max_tokens)) return rc;
+    if (mask_words < 0 || (mask ? mask_words < (max_tokens + 63) / 64 : mask_words != 0) || (uintptr_t)mask % 8 != 0) return BS_EINVAL;
+    if (!workspace || (uintptr_t)workspace % 16 != 0 || workspace_bytes < 0) return BS_EINVAL;
+    if (!rows_aligned(*q, cache->dtype) || !rows_aligned(*out, cache->dtype)) return BS_EUNSUPPORTED;
+    if (int rc = check_rows_apart(*out, n_tokens, cache->head_dim)) return rc;
+    const float to_cap = cap > 0.f ? scale / cap : 0.f;
+    if (cap > 0.f && (!(to_cap > 0.f) || !std::isfinite(to_cap) || !std::isfinite(cap * 1.4426950408889634f) || !(cap * 1.4426950408889634f > 0.f))) return BS_EUNSUPPORTED;
+    int n_cus = 0;
+    Plan p;
+    if (int rc = device_setup(&n_cus)) return rc;
+    if (int rc = make_plan(*cache, q->n_heads, n_tokens, max_tokens, n_cus, &p)) return rc;
+    const int32_t G = q->n_heads / cache->n_kv_heads;
+    // rows of a sequence and KV head are addressed from its first token's in 32 bits
+    if (((__int128)q->token_stride * (std::min(n_tokens, max_tokens) + 1) + (__int128)q->head_stride * G) * element_bytes(cache->dtype) > INT32_MAX) return BS_EUNSUPPORTED;
+    if (workspace_bytes < p.bytes) return BS_EINVAL;
+    if (none) return BS_OK;
+    TreeArgs a{};
+    a.cache = *cache;
+    a.q = q->data; a.q_head = q->head_stride; a.q_token = q->token_stride;
+    a.out = out->data; a.out_head = out->head_stride; a.out_token = out->token_stride;
+    a.first = first;
+    a.lens = lens;
+    a.mask = mask;
+    a.mask_words = mask_words;
+    a.n_tokens = n_tokens;
+    a.max_tokens = std::min(n_tokens, max_tokens);
+    a.G = G;
+    a.window = window;
+    a.most_items = p.most_items;
+    a.scale_log2e = scale * 1.4426950408889634f;
+    a.to_cap = to_cap;
+    a.cap_log2e = cap * 1.4426950408889634f;
+    char *ws = static_cast<char *>(workspace);
+    a.part_o = reinterpret_cast<float *>(ws + p.part_o);
+    a.part_ml = reinterpret_cast<float2 *>(ws + p.part_ml);
+    a.cuts = reinterpret_cast<Cut *>(ws + p.cuts);
+    a.by_item = p.n_cuts < p.n_shares;
+    hipStream_t st = (hipStream_t)stream;
+    if (cache->dtype == BS_BF16) return cache->head_dim == 64 ? launch<__bf16, 64>(a, p, st) : launch<__bf16, 128>(a, p, st);
+    return cache->head_dim == 64 ? launch<float, 64>(a, p, st) : launch<float, 128>(a, p, st);
+}

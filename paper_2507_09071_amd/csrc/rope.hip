@@ -13,6 +13,7 @@
 
 #include "device_map.h"
 #include "paged_cache.h"
+#include "rope_common.h"
 
 namespace bs {
 
@@ -77,56 +78,6 @@ bool rows_aligned(const bs_heads &h, int32_t dtype)
 namespace {
 
 constexpr int kThreads = 256;
-
-// Heads that are rotated or copied.
-struct RopeJob {
-    const void *src;
-    void *dst;
-    int64_t src_head, src_token, dst_head, dst_token;
-    int32_t n_heads;
-    int32_t rotate, paged;   // paged: dst is a pool of pages, dst_token the stride of a slot
-};
-
-struct RopeArgs {
-    RopeJob jobs[3];
-    int32_t n_jobs, n_heads;       // heads of all jobs
-    int32_t n_tokens, groups;      // groups of channels per token that a thread takes
-    int32_t pairs, rotary_dim, head_dim;
-    int32_t head_splits, heads_each;
-    const int32_t *positions;
-    int64_t axis_stride;
-    float magnitude;
-    float direction;               // of the sines: 1 or -1
-    // pages
-    const int32_t *token_seq, *token_slot, *token_order, *page_table;
-    int32_t n_seqs, max_pages, page_size, n_pages, n_kv_heads;
-    int64_t page_stride;
-    float *weights;
-    int32_t *order;
-    int64_t row_stride;
-    double quarter_turns[BS_ROPE_MAX_PAIRS];   // per position: freq * 2 / pi
-    uint8_t axis[BS_ROPE_MAX_PAIRS];
-};
-
-template <typename T, int V>
-struct __align__(sizeof(T) * V) Vec { T x[V]; };
-
-// cos and sin of position * quarter_turns * (pi / 2): the multiple of a quarter turn is taken off in 64 bits, and the rest, at most
-// half a quarter turn, goes through the series of sine and cosine in fp32: the first term left out is below 1.8e-9 (sine) and 1.2e-10 (cosine), what fp32
-// rounds on the way is up to 6.6e-8, about 2^-24.  The 64-bit angle is off by at most 3 |angle| 2^-53: 1e-9 at three million radians, 7e-7 at 2^31.
-__device__ inline void rotation(double quarter_turns, int32_t position, float &c, float &s)
-{
-    const double t = quarter_turns * (double)position, n = rint(t);
-    const float x = (float)((t - n) * 1.5707963267948966);
-    const float x2 = x * x;
-    const float sn = x + x * x2 * fmaf(x2, fmaf(x2, fmaf(x2, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f);
-    const float cs = 1.f + x2 * fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f);
-    const int q = (int)(n - 4.0 * floor(n * 0.25));   // which quarter
-    c = (q & 1) ? sn : cs;
-    s = (q & 1) ? cs : sn;
-    if (q == 1 || q == 2) c = -c;
-    if (q >= 2) s = -s;
-}
 
 // One thread: 2 V channels of one token, of heads_each heads.  Groups 0 .. pairs / V - 1 of a token are V pairs each, the ones behind
 // them 2 V channels that are copied.  (Rows of four heads requested together, before the angles are formed: fewer waves fit, 124 -> 130 us for the
@@ -228,6 +179,40 @@ hipError_t launch_layout(const RopeArgs &a, int vec, hipStream_t st)
 int run_rope(RopeArgs &a, const bs_rope *rope, int32_t dtype, int32_t head_dim, bool inverse, hipStream_t st)
 {
     if (a.n_tokens == 0) return BS_OK;
+    const int vec = fill_rope(a, rope, dtype, head_dim, inverse);
+    // Heads share a thread's angles; where there are too few tokens to fill the chip they are split over threads.
+    const int64_t items = (int64_t)a.n_tokens * a.groups;
+    if (items > INT32_MAX) return BS_EUNSUPPORTED;   // (with several splits there are few, so threads are counted in 32 bits)
+    a.head_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(a.n_heads, (256 * 2048 + items - 1) / items));
+    a.heads_each = (a.n_heads + a.head_splits - 1) / a.head_splits;
+    a.head_splits = (a.n_heads + a.heads_each - 1) / a.heads_each;
+    const bool half = !rope || rope->layout == BS_ROPE_HALF;
+    hipError_t err;
+    if (dtype == BS_BF16) err = half ? launch_layout<__bf16, true>(a, vec, st) : launch_layout<__bf16, false>(a, vec, st);
+    else err = half ? launch_layout<float, true>(a, vec, st) : launch_layout<float, false>(a, vec, st);
+    return err == hipSuccess ? BS_OK : fail_hip(err, "rope_rows launch");
+}
+
+}  // namespace
+
+int check_rope(const bs_rope *r, int32_t n_tokens, int32_t head_dim, const int32_t *positions, int64_t axis_stride)
+{
+    if (!r || (!positions && n_tokens > 0) || axis_stride < 0 || axis_stride > kMaxStride) return BS_EINVAL;
+    if (r->rotary_dim < 2 || r->rotary_dim % 2 != 0 || r->rotary_dim > 2 * BS_ROPE_MAX_PAIRS || r->rotary_dim > head_dim) return BS_EINVAL;
+    if ((r->layout != BS_ROPE_HALF && r->layout != BS_ROPE_INTERLEAVED) || r->n_axes < 1 || r->n_axes > BS_ROPE_MAX_AXES) return BS_EINVAL;
+    if (!std::isfinite(r->magnitude)) return BS_EINVAL;
+    for (int i = 0; i < r->rotary_dim / 2; ++i)
+        if (r->axis[i] >= r->n_axes || !std::isfinite(r->freq[i]) || std::fabs(r->freq[i]) > 1e3) return BS_EINVAL;
+    return BS_OK;
+}
+
+RopeJob job_of(const bs_heads &x, const bs_heads &y, bool rotate)
+{
+    return {x.data, y.data, x.head_stride, x.token_stride, y.head_stride, y.token_stride, x.n_heads, rotate, 0};
+}
+
+int fill_rope(RopeArgs &a, const bs_rope *rope, int32_t dtype, int32_t head_dim, bool inverse)
+{
     a.rotary_dim = rope ? rope->rotary_dim : 0;
     a.pairs = a.rotary_dim / 2;
     a.head_dim = head_dim;
@@ -252,36 +237,51 @@ int run_rope(RopeArgs &a, const bs_rope *rope, int32_t dtype, int32_t head_dim, 
     a.groups = head_dim / (2 * vec);
     a.n_heads = 0;
     for (int j = 0; j < a.n_jobs; ++j) a.n_heads += a.jobs[j].n_heads;
-    // Heads share a thread's angles; where there are too few tokens to fill the chip they are split over threads.
-    const int64_t items = (int64_t)a.n_tokens * a.groups;
-    if (items > INT32_MAX) return BS_EUNSUPPORTED;   // (with several splits there are few, so threads are counted in 32 bits)
-    a.head_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(a.n_heads, (256 * 2048 + items - 1) / items));
-    a.heads_each = (a.n_heads + a.head_splits - 1) / a.head_splits;
-    a.head_splits = (a.n_heads + a.heads_each - 1) / a.heads_each;
-    const bool half = !rope || rope->layout == BS_ROPE_HALF;
-    hipError_t err;
-    if (dtype == BS_BF16) err = half ? launch_layout<__bf16, true>(a, vec, st) : launch_layout<__bf16, false>(a, vec, st);
-    else err = half ? launch_layout<float, true>(a, vec, st) : launch_layout<float, false>(a, vec, st);
-    return err == hipSuccess ? BS_OK : fail_hip(err, "rope_rows launch");
+    return vec;
 }
 
-int check_rope(const bs_rope *r, int32_t n_tokens, int32_t head_dim, const int32_t *positions, int64_t axis_stride)
+int append_args(RopeArgs *a, const bs_cache *cache, const bs_heads *k, const bs_heads *v, int32_t n_tokens, const int32_t *token_seq, const int32_t *token_slot,
+                const bs_rope *rope, const int32_t *positions, int64_t axis_stride, const bs_heads *q, const bs_heads *q_out, const bs_slots *slots,
+                const int32_t *token_order)
 {
-    if (!r || (!positions && n_tokens > 0) || axis_stride < 0 || axis_stride > kMaxStride) return BS_EINVAL;
-    if (r->rotary_dim < 2 || r->rotary_dim % 2 != 0 || r->rotary_dim > 2 * BS_ROPE_MAX_PAIRS || r->rotary_dim > head_dim) return BS_EINVAL;
-    if ((r->layout != BS_ROPE_HALF && r->layout != BS_ROPE_INTERLEAVED) || r->n_axes < 1 || r->n_axes > BS_ROPE_MAX_AXES) return BS_EINVAL;
-    if (!std::isfinite(r->magnitude)) return BS_EINVAL;
-    for (int i = 0; i < r->rotary_dim / 2; ++i)
-        if (r->axis[i] >= r->n_axes || !std::isfinite(r->freq[i]) || std::fabs(r->freq[i]) > 1e3) return BS_EINVAL;
+    if (int rc = check_cache(cache)) return rc;
+    if (n_tokens < 0 || check_heads(k, n_tokens == 0) || check_heads(v, n_tokens == 0) || (!token_slot && n_tokens > 0)) return BS_EINVAL;
+    if (k->n_heads != cache->n_kv_heads || v->n_heads != cache->n_kv_heads || !q != !q_out) return BS_EINVAL;
+    if (q && (check_heads(q, n_tokens == 0) || check_heads(q_out, n_tokens == 0) || q->n_heads != q_out->n_heads || q->n_heads > (1 << 20) || check_rows_apart(*q_out, n_tokens, cache->head_dim))) return BS_EINVAL;
+    if (int rc = check_rows_apart(*cache)) return rc;
+    if (rope)
+        if (int rc = check_rope(rope, n_tokens, cache->head_dim, positions, axis_stride)) return rc;
+    if (slots)
+        if (int rc = check_slots(*cache, slots)) return rc;
+    const int e = element_bytes(cache->dtype);
+    if (((uintptr_t)k->data | (uintptr_t)v->data) % e != 0 || (q && ((uintptr_t)q->data | (uintptr_t)q_out->data) % e != 0)) return BS_EINVAL;
+    if (q) a->jobs[a->n_jobs++] = job_of(*q, *q_out, true);
+    const bs_heads pool_k{cache->k, cache->head_stride, cache->slot_stride, cache->n_kv_heads}, pool_v{cache->v, cache->head_stride, cache->slot_stride, cache->n_kv_heads};
+    a->jobs[a->n_jobs] = job_of(*k, pool_k, rope != nullptr);
+    a->jobs[a->n_jobs++].paged = 1;
+    a->jobs[a->n_jobs] = job_of(*v, pool_v, false);
+    a->jobs[a->n_jobs++].paged = 1;
+    a->n_tokens = n_tokens;
+    a->positions = positions;
+    a->axis_stride = axis_stride;
+    a->token_seq = token_seq;
+    a->token_slot = token_slot;
+    a->token_order = token_order;
+    a->page_table = cache->page_table;
+    a->n_seqs = cache->n_seqs;
+    a->max_pages = cache->max_pages;
+    a->page_size = cache->page_size;
+    a->n_pages = cache->n_pages;
+    a->n_kv_heads = cache->n_kv_heads;
+    a->page_stride = cache->page_stride;
+    if (slots) {
+        a->weights = slots->weights;
+        a->order = slots->order;
+        a->row_stride = slots->row_stride;
+    }
     return BS_OK;
 }
 
-RopeJob job_of(const bs_heads &x, const bs_heads &y, bool rotate)
-{
-    return {x.data, y.data, x.head_stride, x.token_stride, y.head_stride, y.token_stride, x.n_heads, rotate, 0};
-}
-
-}  // namespace
 }  // namespace bs
 
 extern "C" int bs_rope_init(bs_rope *rope, int32_t rotary_dim, int32_t layout, double base, int32_t scaling, double factor,
@@ -351,41 +351,9 @@ extern "C" int bs_cache_append(const bs_cache *cache, const bs_heads *k, const b
                                const bs_heads *q_out, const bs_slots *slots, const int32_t *token_order, void *stream)
 {
     using namespace bs;
-    if (int rc = check_cache(cache)) return rc;
-    if (n_tokens < 0 || check_heads(k, n_tokens == 0) || check_heads(v, n_tokens == 0) || (!token_slot && n_tokens > 0)) return BS_EINVAL;
-    if (k->n_heads != cache->n_kv_heads || v->n_heads != cache->n_kv_heads || !q != !q_out || (q && !rope)) return BS_EINVAL;
-    if (q && (check_heads(q, n_tokens == 0) || check_heads(q_out, n_tokens == 0) || q->n_heads != q_out->n_heads || q->n_heads > (1 << 20) || check_rows_apart(*q_out, n_tokens, cache->head_dim))) return BS_EINVAL;
-    if (int rc = check_rows_apart(*cache)) return rc;
-    if (rope)
-        if (int rc = check_rope(rope, n_tokens, cache->head_dim, positions, axis_stride)) return rc;
-    if (slots)
-        if (int rc = check_slots(*cache, slots)) return rc;
-    const int e = element_bytes(cache->dtype);
-    if (((uintptr_t)k->data | (uintptr_t)v->data) % e != 0 || (q && ((uintptr_t)q->data | (uintptr_t)q_out->data) % e != 0)) return BS_EINVAL;
     RopeArgs a{};
-    if (q) a.jobs[a.n_jobs++] = job_of(*q, *q_out, true);
-    const bs_heads pool_k{cache->k, cache->head_stride, cache->slot_stride, cache->n_kv_heads}, pool_v{cache->v, cache->head_stride, cache->slot_stride, cache->n_kv_heads};
-    a.jobs[a.n_jobs] = job_of(*k, pool_k, rope != nullptr);
-    a.jobs[a.n_jobs++].paged = 1;
-    a.jobs[a.n_jobs] = job_of(*v, pool_v, false);
-    a.jobs[a.n_jobs++].paged = 1;
-    a.n_tokens = n_tokens;
-    a.positions = positions;
-    a.axis_stride = axis_stride;
-    a.token_seq = token_seq;
-    a.token_slot = token_slot;
-    a.token_order = token_order;
-    a.page_table = cache->page_table;
-    a.n_seqs = cache->n_seqs;
-    a.max_pages = cache->max_pages;
-    a.page_size = cache->page_size;
-    a.n_pages = cache->n_pages;
-    a.n_kv_heads = cache->n_kv_heads;
-    a.page_stride = cache->page_stride;
-    if (slots) {
-        a.weights = slots->weights;
-        a.order = slots->order;
-        a.row_stride = slots->row_stride;
-    }
+    if (int rc = check_cache(cache)) return rc;
+    if (q && !rope) return BS_EINVAL;
+    if (int rc = append_args(&a, cache, k, v, n_tokens, token_seq, token_slot, rope, positions, axis_stride, q, q_out, slots, token_order)) return rc;
     return run_rope(a, rope, cache->dtype, cache->head_dim, false, (hipStream_t)stream);
 }
