@@ -5,6 +5,7 @@
 // sum of it.  The bound is HBM: rows are read once and written once (back: two read, one written).
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "device_map.h"
 #include "paged_cache.h"
@@ -17,17 +18,17 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMaxParts = 2048;   // partial sums of the weights' gradients: one per workgroup, eight workgroups on each of 256 CUs
 
 struct NormArgs {
+    int32_t split_end[2];          // where the splits of the first, of the second job end
+    int32_t lane_bits, n_axes;     // lanes of a row: 2^lane_bits
     RopeArgs rope;
     const void *weight[3];         // of each job; null: ones
     int32_t norm[3];               // a job's rows are normed
     int32_t wide;                  // weights in fp32
-    int32_t lane_bits;             // lanes of a row
     float eps, offset, inv_d;
     // the gradient: jobs are x and dx
     const void *dy[2];
     int64_t dy_head[2], dy_token[2];
-    float *parts;                  // [workgroup][job][d]; null: weights are frozen
-    int32_t n_parts;
+    float *parts;                  // [workgroup][d]; null: weights are frozen
     float *dweight;                // [job][d]
 };
 
@@ -51,21 +52,33 @@ struct Channels {
             hi[n] = turns[n] ? lo[n] + (alone ? 1 : a.pairs) : lo[n] + (a.head_dim - a.rotary_dim) / 2;
         }
     }
-    __device__ void angles(const RopeArgs &a, int g0, int t)
+    // All loads of it go out together: the positions on all axes, and which of them turns a pair, do not wait for each other.
+    __device__ void angles(const NormArgs &p, int g0, int t)
     {
+        const RopeArgs &a = p.rope;
+        int32_t at[BS_ROPE_MAX_AXES];
 #pragma unroll
-        for (int n = 0; n < N; ++n)
+        for (int x = 0; x < BS_ROPE_MAX_AXES; ++x) at[x] = a.positions[min(x, p.n_axes - 1) * a.axis_stride + t];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            constexpr bool kWhole = HALF || V == 1;
+            constexpr int H = kWhole ? V : V / 2;   // pairs that lie together: all, or those of lo and those of hi
+            const int i0 = turns[n] ? (kWhole ? (g0 + 64 * n) * V : lo[n] / 2) : 0, i1 = kWhole || !turns[n] ? 0 : hi[n] / 2;
+            double f[V];
+            int x[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                c[n][e] = 1.f;
-                s[n][e] = 0.f;
-                if (turns[n]) {
-                    const int i = HALF || V == 1 ? (g0 + 64 * n) * V + e : (2 * e < V ? lo[n] : hi[n] - V) / 2 + e;
-                    rotation(a.quarter_turns[i], a.positions[a.axis[i] * a.axis_stride + t], c[n][e], s[n][e]);
-                    c[n][e] *= a.magnitude;
-                    s[n][e] *= a.magnitude * a.direction;
-                }
+                const int i = e < H ? i0 + e : i1 + e - H;
+                f[e] = a.quarter_turns[i];
+                x[e] = a.axis[i];
             }
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                rotation(f[e], x[e] == 0 ? at[0] : x[e] == 1 ? at[1] : x[e] == 2 ? at[2] : at[3], c[n][e], s[n][e]);
+                c[n][e] = turns[n] ? c[n][e] * a.magnitude : 1.f;
+                s[n][e] = turns[n] ? s[n][e] * a.magnitude * a.direction : 0.f;
+            }
+        }
     }
     // z: the V channels from lo on, then those from hi on
     __device__ void turn(int n, float (&z)[2 * V]) const
@@ -81,40 +94,61 @@ struct Channels {
     }
 };
 
-template <typename T, int V>
-__device__ inline void load_row(const T *row, int lo, int hi, bool there, float (&z)[2 * V])
-{
-    Vec<T, V> u{}, w{};
-    if (there) {
-        u = *reinterpret_cast<const Vec<T, V> *>(row + lo);
-        w = *reinterpret_cast<const Vec<T, V> *>(row + hi);
-    }
+// A thread's channels of a row as they are in memory.
+template <typename T, int V, int N>
+struct Pieces {
+    Vec<T, V> lo[N], hi[N];
+    template <typename C>
+    __device__ void load(const T *row, const C &ch)
+    {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        z[e] = (float)u.x[e];
-        z[V + e] = (float)w.x[e];
+        for (int n = 0; n < N; ++n) {
+            lo[n] = hi[n] = Vec<T, V>{};
+            if (ch.there[n]) {
+                lo[n] = *reinterpret_cast<const Vec<T, V> *>(row + ch.lo[n]);
+                hi[n] = *reinterpret_cast<const Vec<T, V> *>(row + ch.hi[n]);
+            }
+        }
     }
-}
-
-template <typename T, int V>
-__device__ inline void store_row(T *row, int lo, int hi, const float (&z)[2 * V])
-{
-    Vec<T, V> u, w;
+    template <typename C>
+    __device__ void store(T *row, const C &ch) const
+    {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        u.x[e] = (T)z[e];
-        w.x[e] = (T)z[V + e];
+        for (int n = 0; n < N; ++n)
+            if (ch.there[n]) {
+                *reinterpret_cast<Vec<T, V> *>(row + ch.lo[n]) = lo[n];
+                *reinterpret_cast<Vec<T, V> *>(row + ch.hi[n]) = hi[n];
+            }
     }
-    *reinterpret_cast<Vec<T, V> *>(row + lo) = u;
-    *reinterpret_cast<Vec<T, V> *>(row + hi) = w;
-}
+    __device__ void get(int n, float (&z)[2 * V]) const
+    {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            z[e] = (float)lo[n].x[e];
+            z[V + e] = (float)hi[n].x[e];
+        }
+    }
+    __device__ void set(int n, const float (&z)[2 * V])
+    {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            lo[n].x[e] = (T)z[e];
+            hi[n].x[e] = (T)z[V + e];
+        }
+    }
+};
 
 template <typename W, int V>
 __device__ inline void load_weight_as(const void *weight, int lo, int hi, float (&z)[2 * V])
 {
     const W *w = static_cast<const W *>(weight);
     if ((uintptr_t)w % (sizeof(W) * V) == 0) {
-        load_row<W, V>(w, lo, hi, true, z);
+        const Vec<W, V> u = *reinterpret_cast<const Vec<W, V> *>(w + lo), o = *reinterpret_cast<const Vec<W, V> *>(w + hi);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            z[e] = (float)u.x[e];
+            z[V + e] = (float)o.x[e];
+        }
     } else {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
@@ -136,194 +170,225 @@ __device__ inline void load_weight(const NormArgs &a, int job, int lo, int hi, b
     for (int e = 0; e < 2 * V; ++e) z[e] += a.offset;
 }
 
-// Over the 2^bits lanes of a row.
+// Sum over the 2^bits lanes of a row, in each of them: neighbours, quads, eights and sixteens by data-parallel moves, beyond that by swaps of half rows.
 __device__ inline float row_sum(float x, int bits)
 {
-    for (int off = 1 << bits >> 1; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
+    const auto moved = [](float y, auto control) {
+        return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), decltype(control)::value, 0xf, 0xf, true));
+    };
+    if (bits > 0) x += moved(x, std::integral_constant<int, 0xb1>{});    // lanes 1 0 3 2
+    if (bits > 1) x += moved(x, std::integral_constant<int, 0x4e>{});    // lanes 2 3 0 1
+    if (bits > 2) x += moved(x, std::integral_constant<int, 0x141>{});   // eight lanes reversed
+    if (bits > 3) x += moved(x, std::integral_constant<int, 0x140>{});   // sixteen lanes reversed
+    if (bits > 4) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (bits > 5) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
     return x;
 }
 
-// One thread: its channels of one token, of heads_each heads.
+// 1 / rms, off by at most one unit in the last place (the argument is a normal number: eps is).
+__device__ inline float inverse_rms(float sum, const NormArgs &p) { return __builtin_amdgcn_rsqf(fmaf(row_sum(sum, p.lane_bits), p.inv_d, p.eps)); }
+
+// The job and heads of a split (blockIdx.y).
+struct Share { int job, first, last; };
+__device__ inline Share share_of(const NormArgs &p, int split)
+{
+    Share w;
+    w.job = split < p.split_end[0] ? 0 : split < p.split_end[1] ? 1 : 2;
+    w.first = (split - (w.job > 0 ? p.split_end[w.job - 1] : 0)) * p.rope.heads_each;
+    w.last = min(w.first + p.rope.heads_each, p.rope.jobs[w.job].n_heads);
+    return w;
+}
+
+// One thread: its channels of one token, of heads_each heads of one job (blockIdx.y).  A row is requested while the one before it is turned, the first one before
+// anything else.
 template <typename T, int V, bool HALF, int N>
 __global__ __launch_bounds__(kThreads) void norm_rows(const NormArgs p)
 {
     const RopeArgs &a = p.rope;
-    const uint32_t idx = blockIdx.x * kThreads + threadIdx.x, per_split = (uint32_t)a.n_tokens << p.lane_bits;
-    const int split = (int)(idx / per_split);
-    if (split >= a.head_splits) return;
-    const int item = (int)(idx - split * per_split);
-    const int t = item >> p.lane_bits, g = item & ((1 << p.lane_bits) - 1);
+    const uint32_t item = blockIdx.x * kThreads + threadIdx.x;
+    const int t = (int)(item >> p.lane_bits), g = (int)item & ((1 << p.lane_bits) - 1);
+    if (t >= a.n_tokens) return;
+    const Share w = share_of(p, blockIdx.y);
+    const RopeJob &job = a.jobs[w.job];
     Channels<V, HALF, N> ch;
     ch.place(a, g);
-    ch.angles(a, g, t);
-    // where the token's rows go in the cache
-    int64_t page_at = -1;
-    int at = 0, seq = 0, slot = 0;
-    if (a.token_slot) {
+    const T *src = static_cast<const T *>(job.src) + t * job.src_token + w.first * job.src_head;
+    Pieces<T, V, N> row;
+    row.load(src, ch);
+    // where the token's rows go
+    T *dst = static_cast<T *>(job.dst) + w.first * job.dst_head;
+    int seq = 0, slot = 0;
+    if (job.paged) {
         seq = a.token_seq ? a.token_seq[t] : t;
         slot = a.token_slot[t];
-        if (seq >= 0 && seq < a.n_seqs && slot >= 0 && slot < a.max_pages * a.page_size) {
-            const int page = a.page_table[(int64_t)seq * a.max_pages + slot / a.page_size];
-            at = slot % a.page_size;
-            if (page >= 0 && page < a.n_pages) page_at = page * a.page_stride;
-        }
+        if (seq < 0 || seq >= a.n_seqs || slot < 0 || slot >= a.max_pages * a.page_size) return;
+        const int page = a.page_table[(int64_t)seq * a.max_pages + slot / a.page_size];
+        if (page < 0 || page >= a.n_pages) return;
+        dst += page * a.page_stride + slot % a.page_size * job.dst_token;
+    } else {
+        dst += t * job.dst_token;
     }
-    const int head = split * a.heads_each, end = min(a.n_heads, head + a.heads_each);
-    int first = 0;
-    for (int j = 0; j < a.n_jobs; ++j) {
-        const RopeJob &job = a.jobs[j];
-        const int last = first + job.n_heads;
-        if (max(head, first) < min(end, last) && (!job.paged || page_at >= 0)) {
-            const T *src = static_cast<const T *>(job.src) + t * job.src_token;
-            T *dst = static_cast<T *>(job.dst) + (job.paged ? page_at + at * job.dst_token : t * job.dst_token);
-            float w[N][2 * V];
-            if (p.norm[j]) {
-#pragma unroll
-                for (int n = 0; n < N; ++n) load_weight<V>(p, j, ch.lo[n], ch.hi[n], ch.there[n], w[n]);
-            }
-            for (int h = max(head, first); h < min(end, last); ++h) {
-                const T *x = src + (h - first) * job.src_head;
-                T *y = dst + (h - first) * job.dst_head;
-                if (p.norm[j]) {
-                    float z[N][2 * V], sum = 0.f;
-#pragma unroll
-                    for (int n = 0; n < N; ++n) {
-                        load_row<T, V>(x, ch.lo[n], ch.hi[n], ch.there[n], z[n]);
-#pragma unroll
-                        for (int e = 0; e < 2 * V; ++e) sum = fmaf(z[n][e], z[n][e], sum);
-                    }
-                    const float r = 1.f / sqrtf(fmaf(row_sum(sum, p.lane_bits), p.inv_d, p.eps));
-#pragma unroll
-                    for (int n = 0; n < N; ++n) {
-#pragma unroll
-                        for (int e = 0; e < 2 * V; ++e) z[n][e] *= r * w[n][e];
-                        if (job.rotate) ch.turn(n, z[n]);
-                        if (ch.there[n]) store_row<T, V>(y, ch.lo[n], ch.hi[n], z[n]);
-                    }
-                } else {
-#pragma unroll
-                    for (int n = 0; n < N; ++n)
-                        if (ch.there[n]) {
-                            const Vec<T, V> u = *reinterpret_cast<const Vec<T, V> *>(x + ch.lo[n]), o = *reinterpret_cast<const Vec<T, V> *>(x + ch.hi[n]);
-                            *reinterpret_cast<Vec<T, V> *>(y + ch.lo[n]) = u;
-                            *reinterpret_cast<Vec<T, V> *>(y + ch.hi[n]) = o;
-                        }
-                }
-                if (job.paged && j == a.n_jobs - 1 && g == 0) {   // (V's rows: once per KV head)
-                    const int64_t row = ((int64_t)seq * a.n_kv_heads + (h - first)) * a.row_stride + slot;
-                    if (a.weights) a.weights[row] = 0.f;
-                    if (a.order) a.order[row] = a.token_order ? a.token_order[t] : slot;
-                }
+    if (!p.norm[w.job]) {   // V as it is
+        for (int h = w.first; h < w.last; ++h) {
+            const Pieces<T, V, N> now = row;
+            if (h + 1 < w.last) row.load(src += job.src_head, ch);
+            now.store(dst, ch);
+            dst += job.dst_head;
+            if (g == 0) {   // (once per KV head)
+                const int64_t at = ((int64_t)seq * a.n_kv_heads + h) * a.row_stride + slot;
+                if (a.weights) a.weights[at] = 0.f;
+                if (a.order) a.order[at] = a.token_order ? a.token_order[t] : slot;
             }
         }
-        first = last;
+        return;
+    }
+    float weight[N][2 * V];
+#pragma unroll
+    for (int n = 0; n < N; ++n) load_weight<V>(p, w.job, ch.lo[n], ch.hi[n], ch.there[n], weight[n]);
+    if (job.rotate) ch.angles(p, g, t);
+    for (int h = w.first; h < w.last; ++h) {
+        Pieces<T, V, N> now = row;
+        if (h + 1 < w.last) row.load(src += job.src_head, ch);
+        float z[N][2 * V], sum = 0.f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            now.get(n, z[n]);
+#pragma unroll
+            for (int e = 0; e < 2 * V; ++e) sum = fmaf(z[n][e], z[n][e], sum);
+        }
+        const float r = inverse_rms(sum, p);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+#pragma unroll
+            for (int e = 0; e < 2 * V; ++e) z[n][e] *= r * weight[n][e];
+            if (job.rotate) ch.turn(n, z[n]);
+            now.set(n, z[n]);
+        }
+        now.store(dst, ch);
+        dst += job.dst_head;
     }
 }
 
-// One thread: its channels of one token at a time, of heads_each heads; it adds up its part of the weights' gradients over all of them.
+// One thread: its channels of one token at a time, of heads_each heads of one job (blockIdx.y); it adds up its part of the weight's gradient over all of them.
 template <typename T, int V, bool HALF, int N>
 __global__ __launch_bounds__(kThreads) void norm_grad_rows(const NormArgs p)
 {
     const RopeArgs &a = p.rope;
-    __shared__ float sums[kWaves][2][2 * BS_ROPE_MAX_PAIRS];
-    const uint32_t per_split = (uint32_t)a.n_tokens << p.lane_bits;
+    __shared__ float sums[kWaves][2 * BS_ROPE_MAX_PAIRS];
     const int g = threadIdx.x & ((1 << p.lane_bits) - 1);
+    const Share w = share_of(p, blockIdx.y);
+    const RopeJob &job = a.jobs[w.job];
     Channels<V, HALF, N> ch;
     ch.place(a, g);
-    float w[2][N][2 * V], dw[2][N][2 * V];
+    float weight[N][2 * V], dw[N][2 * V];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int n = 0; n < N; ++n) {
+        load_weight<V>(p, w.job, ch.lo[n], ch.hi[n], ch.there[n], weight[n]);
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            if (j < a.n_jobs) load_weight<V>(p, j, ch.lo[n], ch.hi[n], ch.there[n], w[j][n]);
+        for (int e = 0; e < 2 * V; ++e) dw[n][e] = 0.f;
+    }
+    for (uint64_t item = (uint64_t)blockIdx.x * kThreads + threadIdx.x; item >> p.lane_bits < (uint64_t)a.n_tokens; item += (uint64_t)gridDim.x * kThreads) {
+        const int t = (int)(item >> p.lane_bits);
+        const T *src = static_cast<const T *>(job.src) + t * job.src_token + w.first * job.src_head;
+        const T *dys = static_cast<const T *>(p.dy[w.job]) + t * p.dy_token[w.job] + w.first * p.dy_head[w.job];
+        T *dst = static_cast<T *>(job.dst) + t * job.dst_token + w.first * job.dst_head;
+        Pieces<T, V, N> row, dy;
+        row.load(src, ch);
+        dy.load(dys, ch);
+        if (job.rotate) ch.angles(p, g, t);
+        for (int h = w.first; h < w.last; ++h) {
+            Pieces<T, V, N> now = row;
+            const Pieces<T, V, N> grad = dy;
+            if (h + 1 < w.last) {
+                row.load(src += job.src_head, ch);
+                dy.load(dys += p.dy_head[w.job], ch);
+            }
+            float x[N][2 * V], u[N][2 * V], square = 0.f, dot = 0.f;
 #pragma unroll
-            for (int e = 0; e < 2 * V; ++e) dw[j][n][e] = 0.f;
-        }
-    for (uint64_t idx = (uint64_t)blockIdx.x * kThreads + threadIdx.x; idx < (uint64_t)per_split * a.head_splits; idx += (uint64_t)gridDim.x * kThreads) {
-        const int split = (int)(idx / per_split), t = (int)(idx - (uint64_t)split * per_split) >> p.lane_bits;
-        ch.angles(a, g, t);
-        const int head = split * a.heads_each, end = min(a.n_heads, head + a.heads_each);
-        int first = 0;
+            for (int n = 0; n < N; ++n) {
+                now.get(n, x[n]);
+                grad.get(n, u[n]);
+                if (job.rotate) ch.turn(n, u[n]);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            if (j >= a.n_jobs) break;
-            const RopeJob &job = a.jobs[j];
-            const int last = first + job.n_heads;
-            const T *src = static_cast<const T *>(job.src) + t * job.src_token, *dys = static_cast<const T *>(p.dy[j]) + t * p.dy_token[j];
-            T *dst = static_cast<T *>(job.dst) + t * job.dst_token;
-            for (int h = max(head, first); h < min(end, last); ++h) {
-                float x[N][2 * V], u[N][2 * V], square = 0.f, dot = 0.f;
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    load_row<T, V>(src + (h - first) * job.src_head, ch.lo[n], ch.hi[n], ch.there[n], x[n]);
-                    load_row<T, V>(dys + (h - first) * p.dy_head[j], ch.lo[n], ch.hi[n], ch.there[n], u[n]);
-                }
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    ch.turn(n, u[n]);
-#pragma unroll
-                    for (int e = 0; e < 2 * V; ++e) {
-                        square = fmaf(x[n][e], x[n][e], square);
-                        dot = fmaf(u[n][e] * w[j][n][e], x[n][e], dot);
-                    }
-                }
-                const float r = 1.f / sqrtf(fmaf(row_sum(square, p.lane_bits), p.inv_d, p.eps));
-                const float k = row_sum(dot, p.lane_bits) * p.inv_d * r * r;   // mean(u v) r
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    float z[2 * V];
-#pragma unroll
-                    for (int e = 0; e < 2 * V; ++e) {
-                        z[e] = r * fmaf(-x[n][e], k, u[n][e] * w[j][n][e]);
-                        dw[j][n][e] = fmaf(u[n][e], x[n][e] * r, dw[j][n][e]);
-                    }
-                    if (ch.there[n]) store_row<T, V>(dst + (h - first) * job.dst_head, ch.lo[n], ch.hi[n], z);
+                for (int e = 0; e < 2 * V; ++e) {
+                    square = fmaf(x[n][e], x[n][e], square);
+                    dot = fmaf(u[n][e] * weight[n][e], x[n][e], dot);
                 }
             }
-            first = last;
+            const float r = inverse_rms(square, p);
+            const float k = row_sum(dot, p.lane_bits) * p.inv_d * r * r;   // mean(u v) r
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                float z[2 * V];
+#pragma unroll
+                for (int e = 0; e < 2 * V; ++e) {
+                    z[e] = r * fmaf(-x[n][e], k, u[n][e] * weight[n][e]);
+                    dw[n][e] = fmaf(u[n][e], x[n][e] * r, dw[n][e]);
+                }
+                now.set(n, z);
+            }
+            now.store(dst, ch);
+            dst += job.dst_head;
         }
     }
     if (!p.parts) return;
     // over the rows of a wave, then the waves: always in the same order
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int n = 0; n < N; ++n)
-#pragma unroll
-            for (int e = 0; e < 2 * V; ++e) {
-                float x = dw[j][n][e];
-                for (int off = 1 << p.lane_bits; off < 64; off <<= 1) x += __shfl_xor(x, off, 64);
-                if (lane == g && ch.there[n]) sums[threadIdx.x >> 6][j][(e < V ? ch.lo[n] + e : ch.hi[n] + e - V)] = x;
-            }
+        for (int e = 0; e < 2 * V; ++e) {
+            float x = dw[n][e];
+            for (int off = 1 << p.lane_bits; off < 64; off <<= 1) x += __shfl_xor(x, off, 64);
+            if (lane == g && ch.there[n]) sums[threadIdx.x >> 6][e < V ? ch.lo[n] + e : ch.hi[n] + e - V] = x;
+        }
     __syncthreads();
-    for (int i = threadIdx.x; i < a.n_jobs * a.head_dim; i += kThreads) {
-        const int j = i / a.head_dim, c = i - j * a.head_dim;
+    for (int c = threadIdx.x; c < a.head_dim; c += kThreads) {
         float x = 0.f;
 #pragma unroll
-        for (int v = 0; v < kWaves; ++v) x += sums[v][j][c];
-        (p.n_parts == 1 ? p.dweight : p.parts + (int64_t)blockIdx.x * a.n_jobs * a.head_dim)[i] = x;
+        for (int v = 0; v < kWaves; ++v) x += sums[v][c];
+        p.parts[((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * a.head_dim + c] = x;
     }
 }
 
-// Sums of the workgroups, in 64 bits and always in the same order: a workgroup takes 16 of the n_jobs d channels, 64 threads each.
-__global__ __launch_bounds__(1024) void norm_grad_join(const float *__restrict__ parts, int n_parts, int n, float *__restrict__ dweight)
+// Sums of the workgroups, in 64 bits and always in the same order: a workgroup takes 16 channels of a job (blockIdx.y), in pieces of two, 128 threads for each.
+__global__ __launch_bounds__(1024) void norm_grad_join(const float *__restrict__ parts, int per_split, int splits0, int splits, int d, float *__restrict__ dweight)
 {
-    __shared__ double sums[64][16];
-    const int c = threadIdx.x & 15, v = threadIdx.x >> 4, i = blockIdx.x * 16 + c;
-    double x = 0.0;
-    for (int k0 = v; k0 < n_parts; k0 += 8 * 64) {   // loads of eight parts go out together
-        float y[8];
+    __shared__ double sums[16][16];
+    const int job = blockIdx.y, c = blockIdx.x * 16 + (threadIdx.x & 7) * 2, v = threadIdx.x >> 3, wave = threadIdx.x >> 6;
+    const int begin = (job == 0 ? 0 : splits0) * per_split, end = (job == 0 ? splits0 : splits) * per_split;
+    double x = 0.0, y = 0.0;
+    for (int k0 = begin + v; k0 < end; k0 += 16 * 128) {   // loads of sixteen parts go out together
+        float2 z[16];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] = i < n && k0 + 64 * k < n_parts ? parts[(int64_t)(k0 + 64 * k) * n + i] : 0.f;
+        for (int k = 0; k < 16; ++k) z[k] = c < d && k0 + 128 * k < end ? *reinterpret_cast<const float2 *>(parts + (int64_t)(k0 + 128 * k) * d + c) : make_float2(0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x += y[k];
+        for (int k = 0; k < 16; ++k) {
+            x += z[k].x;
+            y += z[k].y;
+        }
     }
-    sums[v][c] = x;
+#pragma unroll
+    for (int off = 8; off < 64; off <<= 1) {
+        x += __shfl_xor(x, off, 64);
+        y += __shfl_xor(y, off, 64);
+    }
+    if ((threadIdx.x & 63) < 8) {
+        sums[wave][(threadIdx.x & 7) * 2] = x;
+        sums[wave][(threadIdx.x & 7) * 2 + 1] = y;
+    }
     __syncthreads();
-    if (v > 0 || i >= n) return;
-    for (int k = 1; k < 64; ++k) x += sums[k][c];
-    dweight[i] = (float)x;
+    const int out = blockIdx.x * 16 + threadIdx.x;
+    if (threadIdx.x >= 16 || out >= d) return;
+    x = 0.0;
+    for (int k = 0; k < 16; ++k) x += sums[k][threadIdx.x];
+    dweight[job * d + out] = (float)x;
 }
 
 template <typename T, int V, bool HALF, int N>
@@ -364,27 +429,36 @@ int run_norm(NormArgs &p, const bs_norm &norm, const bs_rope *rope, int32_t dtyp
     p.eps = norm.eps;
     p.offset = norm.offset;
     p.inv_d = 1.f / head_dim;
-    // Heads share a thread's angles and weights; where there are too few tokens to fill the chip they are split over threads.
+    p.n_axes = rope ? rope->n_axes : 1;
+    // Heads of a job share a thread's angles and weights; where there are too few tokens to fill the chip they are split over threads.  Forward: half a million threads
+    // (39.5K tokens of 28 + 4 heads 122 us, with a quarter of a million 128), but where that many are there anyway, two heads each, the second of which is requested
+    // ahead (847 tokens of 40 + 8 + 8 heads into the cache: 11.2 -> 9.0 us).  Back, where a thread has three times the registers: an eighth of a million (5K tokens, 32 + 16
+    // heads in fp32: 79 -> 77 us, and fewer parts to join).
     const int64_t items = (int64_t)a.n_tokens << p.lane_bits;
-    if (items > INT32_MAX) return BS_EUNSUPPORTED;   // (with several splits there are few, so threads are counted in 32 bits)
+    if (items > INT32_MAX) return BS_EUNSUPPORTED;
     hipError_t err = hipSuccess;
+    int splits[3] = {0, 0, 0};   // up to and with each job
+    dim3 grid(0);
     if (items > 0) {
-        a.head_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(a.n_heads, (256 * 2048 + items - 1) / items));
+        const auto for_threads = [&](int64_t n) { return (n + items - 1) / items; };
+        int64_t want = for_threads(gradient ? 131072 : 524288);
+        if (!gradient) want = std::min(want, std::max<int64_t>(for_threads(131072), (a.n_heads + 1) / 2));
+        a.head_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(a.n_heads, 1024), want));
         a.heads_each = (a.n_heads + a.head_splits - 1) / a.head_splits;
-        a.head_splits = (a.n_heads + a.heads_each - 1) / a.heads_each;
-        int64_t wgs = (items * a.head_splits + kThreads - 1) / kThreads;
-        if (gradient) wgs = std::min<int64_t>(wgs, kMaxParts);
-        p.n_parts = (int32_t)std::min<int64_t>(wgs, kMaxParts);
+        for (int j = 0; j < 3; ++j) splits[j] = (j > 0 ? splits[j - 1] : 0) + (j < a.n_jobs ? (a.jobs[j].n_heads + a.heads_each - 1) / a.heads_each : 0);
+        a.head_splits = splits[2];   // (at most 1026)
+        p.split_end[0] = splits[0];
+        p.split_end[1] = splits[1];
+        int64_t wgs = (items + kThreads - 1) / kThreads;
+        if (gradient) wgs = std::max<int64_t>(1, std::min<int64_t>(wgs, kMaxParts / a.head_splits));
+        grid = dim3((unsigned)wgs, (unsigned)a.head_splits);
         const bool half = !rope || rope->layout == BS_ROPE_HALF;
-        const dim3 grid((unsigned)wgs);
         if (dtype == BS_BF16) err = half ? launch_layout<__bf16, true>(p, vec, gradient, grid, st) : launch_layout<__bf16, false>(p, vec, gradient, grid, st);
         else err = half ? launch_layout<float, true>(p, vec, gradient, grid, st) : launch_layout<float, false>(p, vec, gradient, grid, st);
         if (err != hipSuccess) return fail_hip(err, "norm_rows launch");
     }
-    if (gradient && p.dweight && p.n_parts != 1) {   // (no tokens: sums of nothing)
-        const int n = a.n_jobs * head_dim;
-        err = launch_kernel(norm_grad_join, dim3((unsigned)((n + 15) / 16)), dim3(1024), 0, st, p.parts, p.n_parts, n, p.dweight);
-    }
+    if (gradient && p.dweight)   // (no tokens: sums of nothing)
+        err = launch_kernel(norm_grad_join, dim3((unsigned)((head_dim + 15) / 16), (unsigned)a.n_jobs), dim3(1024), 0, st, p.parts, (int)grid.x, splits[0], splits[2], head_dim, p.dweight);
     return err == hipSuccess ? BS_OK : fail_hip(err, "norm_grad_join launch");
 }
 

@@ -111,9 +111,9 @@ def check_forward(xs, ws, rope, positions, dtype, eps=1e-6, offset=0.0, views=No
 def chain(n_heads, n_tokens, lanes):
     """Rows that a thread adds up at most: its heads of each token that it has."""
     items = n_tokens * lanes
-    splits = max(1, min(n_heads, -(-256 * 2048 // items)))
-    each = -(-n_heads // splits)
-    return each * -(-items * -(-n_heads // each) // (2048 * 256))
+    splits = max(1, min(n_heads, -(-131072 // items)))
+    workgroups = max(1, min(-(-items // 256), 2048 // (splits + 2)))
+    return -(-n_heads // splits) * -(-items // (workgroups * 256))
 
 
 def check_grad(xs, dys, ws, rope, positions, dtype, eps=1e-6, offset=0.0, views=None, in_place=None, weights=True):
