@@ -36,6 +36,7 @@ struct TreeArgs {
     const uint64_t *mask;
     int32_t n_tokens, max_tokens, mask_words;
     int32_t G, window, most_items;   // heads per KV head; items of a sequence at most
+    float inv_g;                  // 1 / G
     float scale_log2e;            // of scores as they are, or
     float to_cap, cap_log2e;      // cap > 0: scale / cap, cap log2(e)
     float *part_o;                // [2 shares][M][d]: of share w, 2 w the item that began before it, 2 w + 1 the one that goes on behind it
@@ -47,14 +48,14 @@ struct TreeArgs {
 // NRB blocks of 16 rows per wave, WR waves that share a block of slots, WK such groups of waves that take turns.
 template <typename T, int D, int NRB, int WR, int WK>
 struct Layout {
-    static constexpr int kWaves = WR * WK, kThreads = 64 * kWaves, kRows = 16 * NRB * WR;
+    static constexpr int kWaves = WR * WK, kThreads = 64 * kWaves, kRows = 16 * NRB * WR, kTurns = WK;
     static constexpr int kKeys = sizeof(T) == 2 ? 32 : 16;    // slots of a block
     static constexpr int kRowBytes = D * (int)sizeof(T);
     static constexpr int kBlock = kKeys * kRowBytes;          // one block of K or V
     static constexpr int kLoads = kBlock / 1024;              // LDS-direct instructions per block
     static constexpr int kLoads16 = 16 * kRowBytes / 1024;    // ... per 16 slots, which lie in one page
     static constexpr int kOwn = (kLoads + WR - 1) / WR;       // ... of a wave
-    static constexpr int kStages = WR > 1 && WK <= 2 && sizeof(T) == 2 ? 3 : 2;
+    static constexpr int kStages = 2;
     static constexpr int kGroup = kStages * 2 * kBlock;       // ring of a group of waves
     static constexpr int kQuery = WK * kGroup;                // the query rows behind the rings
     static constexpr int kMerge = WR > 1 ? kRows * D * 4 : kGroup;   // a group's results lie over the ring; where its waves have it alone, over its own part
@@ -72,6 +73,8 @@ struct Layout {
 
 // Beginning an item costs about as much as so many blocks: shares are equal with that counted.
 constexpr int kItemBlocks = 4;
+
+typedef float floatx8 __attribute__((ext_vector_type(8)));
 
 // A sequence: slots in use, its drafted tokens; what is visible of it, from block `first` on; units: of an item, with its beginning; items of it.
 struct Seq { int base, token, T, n, begin, first, blocks, units, groups, items; };
@@ -93,6 +96,9 @@ __device__ inline Seq seq_of(const TreeArgs &a, int s, LOAD load)
     v.units = v.T > 0 ? v.blocks + kItemBlocks : 0;
     return v;
 }
+// Row R of a sequence and KV head is token R / G.  (R + 1/2) / G is at least 1 / (2 G) away from whole numbers, and off by less than that for R below 2^21.
+__device__ inline int token_of(const TreeArgs &a, int R) { return (int)(((float)R + 0.5f) * a.inv_g); }
+
 struct ScalarLoad { __device__ int operator()(const int32_t *p) const { return scalar_load<int>(p); } };
 struct VectorLoad { __device__ int operator()(const int32_t *p) const { return *p; } };
 
@@ -168,18 +174,86 @@ __device__ inline Range own_range(const TreeArgs &a, int share, int n_shares)
     return r;
 }
 
-// cap tanh(x scale / cap) log2(e).  Below 1 the quotient that the continued fraction of tanh gives after six terms (relative error 3e-9), from there on (e - 1) / (e + 1)
-// with e = exp(2 x): neither loses anything to a difference of numbers that are alike.  (Beyond 15 tanh is 1 to the last bit.)
-__device__ inline float capped(const TreeArgs &a, float s)
+// tanh, in place, of scores times to_cap.  Below 1 a quotient of polynomials, the continued fraction of tanh after five terms (relative error 6e-8, at 1); capped scores are
+// that small as a rule, so it is tried alone, without the exponential.  From 1 on (e - 1) / (e + 1), e = exp(2 x): neither loses anything to a difference of
+// numbers that are alike.  (Beyond 15 tanh is 1 to the last bit; a NaN stays one.)
+template <typename V, int N>
+__device__ inline void tanh_scores(V (&s)[N], float to_cap)
 {
-    float x = s * a.to_cap;
-    x = x > 15.f ? 15.f : x;
-    x = x < -15.f ? -15.f : x;   // (a NaN stays one)
-    const float x2 = x * x, e = __builtin_amdgcn_exp2f(x * 2.8853900817779268f);
-    const bool small = x2 < 1.f;
-    const float num = small ? x * fmaf(x2, fmaf(x2, 21.f, 1260.f), 10395.f) : e - 1.f;
-    const float den = small ? fmaf(x2, fmaf(x2, x2 + 210.f, 4725.f), 10395.f) : e + 1.f;
-    return num * __builtin_amdgcn_rcpf(den) * a.cap_log2e;
+    constexpr int E = sizeof(V) / 4;
+    float most = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            s[n][e] *= to_cap;
+            most = fmaxf(most, fabsf(s[n][e]));
+        }
+    const bool small = __all(most < 1.f);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float x = s[n][e], x2 = x * x;
+            float num = x * fmaf(x2, x2 + 105.f, 945.f), den = fmaf(x2, fmaf(x2, 15.f, 420.f), 945.f);
+            if (!small) {
+                const float y = x > 15.f ? 15.f : x < -15.f ? -15.f : x, z = __builtin_amdgcn_exp2f(y * 2.8853900817779268f);
+                num = x2 < 1.f ? num : z - 1.f;
+                den = x2 < 1.f ? den : z + 1.f;
+            }
+            s[n][e] = num * __builtin_amdgcn_rcpf(den);
+        }
+}
+
+// What the rows of an item see of the drafted tokens, [8 words][ROWS], and where a window begins, [ROWS], into LDS.  Threads tid of THREADS.
+template <int ROWS, int THREADS>
+__device__ inline void rows_see(const TreeArgs &a, const Seq &seq, int row0, int n_rows, uint32_t *masks, int *begins, int tid)
+{
+    for (int r = tid; r < ROWS; r += THREADS) {
+        const int t = token_of(a, row0 + min(r, n_rows - 1));
+        uint64_t words[BS_TREE_MAX_TOKENS / 64];
+        int seen = 0;
+#pragma unroll
+        for (int w = 0; w < BS_TREE_MAX_TOKENS / 64; ++w) {
+            uint64_t x = a.mask ? 0 : bits_between(0, t + 1 - 64 * w);
+            if (a.mask && w < a.mask_words) x = a.mask[(int64_t)(seq.token + t) * a.mask_words + w];
+            words[w] = x & bits_between(0, seq.T - 64 * w);
+            seen += __popcll(words[w]);
+        }
+        int begin = 0;
+        if (a.window > 0) {
+            begin = max(0, seq.base - max(0, a.window - seen));
+            int drop = seen - a.window;   // the first ones
+#pragma unroll
+            for (int w = 0; w < BS_TREE_MAX_TOKENS / 64; ++w) {
+                const int n = __popcll(words[w]);
+                if (drop >= n) words[w] = 0;
+                else for (int i = 0; i < drop; ++i) words[w] &= words[w] - 1;
+                drop -= n;
+            }
+        }
+#pragma unroll
+        for (int w = 0; w < 8; ++w) masks[w * ROWS + r] = (uint32_t)(words[w / 2] >> (32 * (w % 2)));
+        begins[r] = begin;
+    }
+}
+
+// 32 slots from n0 on that a row sees.
+template <int ROWS>
+__device__ inline uint32_t row_sees(const uint32_t *masks, const int *begins, int row, int n0, int base)
+{
+    const int rel = n0 - base;   // drafted token of the first slot
+    uint32_t x;
+    if (rel >= 0) {
+        const int w = min(rel >> 5, 8);
+        const uint32_t lo = w < 8 ? masks[w * ROWS + row] : 0, hi = w < 7 ? masks[(w + 1) * ROWS + row] : 0;
+        x = __builtin_amdgcn_alignbit(hi, lo, rel & 31);
+    } else {
+        x = rel > -32 ? (masks[row] << (-rel & 31)) | ~(~0u << (-rel & 31)) : ~0u;
+    }
+    const int before = begins[row] - n0;   // slots that lie before the row's window
+    if (before > 0) x &= before < 32 ? ~0u << before : 0u;
+    return x;
 }
 
 template <typename T, int D, int NRB, int WR, int WK>
@@ -308,7 +382,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
                 const int i = i0 + wave;
                 if (kAll % WAVES == 0 || i < kAll) {
                     const int r = i * (1024 / ROWB) + lane / (ROWB / 16), p = lane % (ROWB / 16);
-                    const int R = row0 + min(r, n_rows - 1), t = R / a.G;
+                    const int R = row0 + min(r, n_rows - 1), t = token_of(a, R);
                     load_lds((uint32_t)((t * a.q_token + (R - t * a.G) * a.q_head) * (int64_t)sizeof(T)) + ((p ^ TR::swizzle(r)) << 4), qh, lds0 + TR::kQuery + i * 1024);
                 }
             }
@@ -327,34 +401,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
                 issue(s1.v, ring + 3 * BLK);
             }
         }
-        // What the rows see of the drafted tokens, and where a window begins
-        for (int r = tid; r < ROWS; r += THREADS) {
-            const int t = (row0 + min(r, n_rows - 1)) / a.G;
-            uint64_t words[BS_TREE_MAX_TOKENS / 64];
-            int seen = 0;
-#pragma unroll
-            for (int w = 0; w < BS_TREE_MAX_TOKENS / 64; ++w) {
-                uint64_t x = a.mask ? 0 : bits_between(0, t + 1 - 64 * w);
-                if (a.mask && w < a.mask_words) x = a.mask[(int64_t)(seq.token + t) * a.mask_words + w];
-                words[w] = x & bits_between(0, seq.T - 64 * w);
-                seen += __popcll(words[w]);
-            }
-            int begin = 0;
-            if (a.window > 0) {
-                begin = max(0, seq.base - max(0, a.window - seen));
-                int drop = seen - a.window;   // the first ones
-#pragma unroll
-                for (int w = 0; w < BS_TREE_MAX_TOKENS / 64; ++w) {
-                    const int n = __popcll(words[w]);
-                    if (drop >= n) words[w] = 0;
-                    else for (int i = 0; i < drop; ++i) words[w] &= words[w] - 1;
-                    drop -= n;
-                }
-            }
-#pragma unroll
-            for (int w = 0; w < 8; ++w) reinterpret_cast<uint32_t *>(lds + TR::kMask)[w * ROWS + r] = (uint32_t)(words[w / 2] >> (32 * (w % 2)));
-            reinterpret_cast<int *>(lds + TR::kBegin)[r] = begin;
-        }
+        rows_see<ROWS, THREADS>(a, seq, row0, n_rows, reinterpret_cast<uint32_t *>(lds + TR::kMask), reinterpret_cast<int *>(lds + TR::kBegin), tid);
         if (!SHARED && n_steps > 1) wait_loads(std::integral_constant<int, 4 * NI>{});
         else if (!SHARED && n_steps == 1) wait_loads(std::integral_constant<int, 2 * NI>{});
         else wait_loads(std::integral_constant<int, 0>{});
@@ -378,7 +425,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[rb][nb][i] = 0.f;
         }
-        const float c = a.cap_log2e > 0.f ? 1.f : a.scale_log2e;   // of scores that are not capped
+        const float c = a.cap_log2e > 0.f ? a.cap_log2e : a.scale_log2e;
         // Slots below this one, if their pages are there, are seen by all rows, but for those before the window's last begin.
         const int window_end = a.window > 0 ? min(seq.base, seq.base - a.window + seq.T) : 0;
 
@@ -445,11 +492,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
             }
             if (a.cap_log2e > 0.f) {
 #pragma unroll
-                for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-                    for (int h = 0; h < SUB; ++h)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) s[rb][h][e] = capped(a, s[rb][h][e]);
+                for (int rb = 0; rb < NRB; ++rb) tanh_scores(s[rb], a.to_cap);
             }
 
             // ---- which of the lane's slots its rows see (4 bits per 16 slots)
@@ -462,17 +505,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
             if (masked) {
 #pragma unroll
                 for (int rb = 0; rb < NRB; ++rb) {
-                    const int row = (wr * NRB + rb) * 16 + col, rel = n0 - seq.base;   // drafted token of the first slot
-                    uint32_t x;
-                    if (rel >= 0) {
-                        const int w = min(rel >> 5, 8);
-                        const uint32_t lo = w < 8 ? row_mask[w * ROWS + row] : 0, hi = w < 7 ? row_mask[(w + 1) * ROWS + row] : 0;
-                        x = __builtin_amdgcn_alignbit(hi, lo, rel & 31);
-                    } else {
-                        x = rel > -32 ? (row_mask[row] << (-rel & 31)) | ~(~0u << (-rel & 31)) : ~0u;
-                    }
-                    const int before = row_begin[row] - n0;   // slots that lie before the row's window
-                    if (before > 0) x &= before < 32 ? ~0u << before : 0u;
+                    const uint32_t x = row_sees<ROWS>(row_mask, row_begin, (wr * NRB + rb) * 16 + col, n0, seq.base);
                     seen[rb] = (x & exists) >> (4 * grp);
 #pragma unroll
                     for (int h = 0; h < SUB; ++h)
@@ -664,12 +697,363 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
             }
             if (begins && ends) {
                 const float inv = l == 0.f ? 0.f : 1.f / l;
-                const int R = row0 + row, t = R / a.G;
+                const int R = row0 + row, t = token_of(a, R);
                 store_row4(static_cast<T *>(a.out) + (seq.token + t) * a.out_token + (int64_t)(kvh * a.G + R - t * a.G) * a.out_head + 4 * ch,
                            make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
             } else {
                 *reinterpret_cast<float4 *>(a.part_o + (part + row) * D + 4 * ch) = sum;
                 if (ch == 0) a.part_ml[part + row] = make_float2(m, l);
+            }
+        }
+        if (begins && tid == 0 && (a.by_item || !ends))
+            a.cuts[a.by_item ? at.seq * a.most_items + at.item : (int)blockIdx.x] = Cut{at.seq, at.item, (int)blockIdx.x, (pos - at.unit + seq.units - 1) / range.each};
+        pos += seq.units - at.unit;   // (behind the share's end if the item is cut)
+        at.unit = 0;
+        ++at.item;
+        if (pos < range.end) __syncthreads();   // the LDS is free again
+    }
+}
+
+// Many rows (bf16): four waves of 32 rows each walk the same blocks of 32 slots in step; two such workgroups share a CU.
+template <int D>
+struct Wide {
+    static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves, kKeys = 32, kTurns = 1, kPerCu = 2;
+    static constexpr int kRowBytes = 2 * D, kBlock = kKeys * kRowBytes;                        // a block of K or V
+    static constexpr int kLoads16 = 16 * kRowBytes / 1024;    // LDS-direct instructions per 16 slots, which lie in one page
+    static constexpr int kSlots = D == 64 ? 8 : 4;            // blocks of K, of V, that the LDS holds
+    static constexpr int kValues = kSlots * kBlock;           // V's ring behind K's; at first the query rows, until they are in registers
+    static constexpr int kMerge = kRows * D * 4;              // results lie over the rings
+    static constexpr int kEnd = 2 * kValues > kMerge ? 2 * kValues : kMerge;
+    static constexpr int kMask = kEnd, kBegin = kMask + 8 * kRows * 4, kMl = kBegin + kRows * 4;
+    static constexpr int kThere = kMl + kRows * 8;            // [ring][2]: 16 slots have a page
+    static constexpr int kBad = kThere + kSlots * 8;          // [ring]: slots with a value that is not finite
+    static constexpr int kLds = kBad + kSlots * 4;
+    static_assert((kLds + 1024) * kPerCu <= 160 * 1024, "LDS of a CU");
+    static_assert(kRows * kRowBytes <= kValues, "query rows");
+    // exchange of the 16-byte chunks of row r: rows that share their banks get different chunks.  K is read 16 rows of a chunk at a time, V four rows of four chunks.
+    __device__ static int swizzle(int r) { return kRowBytes == 128 ? (r >> 1) & 7 : r & 15; }
+    __device__ static int swizzle_v(int r) { return kRowBytes == 128 ? (r & 2) << 1 | ((r >> 2) & 3) : (r & 3) << 2 | ((r >> 2) & 3); }
+};
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
+{
+    using TR = Wide<D>;
+    constexpr int KEYS = TR::kKeys, ROWB = TR::kRowBytes, BLK = TR::kBlock, NI16 = TR::kLoads16, ROWS = TR::kRows, THREADS = TR::kThreads, RING = TR::kSlots;
+    constexpr int KSTEPS = D / 16, CB = D / 32, CH4 = D / 4;
+    extern __shared__ __align__(1024) unsigned char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, n31 = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int P16 = a.cache.page_size / 16;
+    const int64_t page_bytes = a.cache.page_stride * 2, slots16_bytes = a.cache.slot_stride * 32;
+
+    if (a.by_item)   // items that a sequence could have and has not: nothing to join
+        for (int s = blockIdx.x; s < a.cache.n_seqs; s += gridDim.x)
+            for (int i = seq_of<KEYS, ROWS>(a, s, ScalarLoad{}).items + tid; i < a.most_items; i += THREADS) a.cuts[s * a.most_items + i] = Cut{s, i, 0, 0};
+    const Range range = own_range<KEYS, ROWS, 1, THREADS>(a, blockIdx.x, gridDim.x);
+    if (tid == 0 && !a.by_item) a.cuts[blockIdx.x] = Cut{0, -1, 0, 0};
+    if (range.begin >= range.end) return;
+
+    typedef __attribute__((address_space(3))) void *lds_ptr;
+    typedef __attribute__((address_space(3))) bf16x4 *lds_bf16x4;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr)lds;
+    // What the wave loads of a block: 16 of its slots, K or V
+    const int sub = wave & 1;
+    const bool values = wave & 2;
+    const char *pool = static_cast<const char *>(values ? a.cache.v : a.cache.k);
+    const uint32_t to0 = lds0 + (values ? TR::kValues : 0) + sub * 16 * ROWB;
+    uint32_t voff[NI16];   // as in tree_shares
+#pragma unroll
+    for (int x = 0; x < NI16; ++x) {
+        const int r = x * (1024 / ROWB) + lane / (ROWB / 16), p = lane % (ROWB / 16);
+        voff[x] = r * (uint32_t)(a.cache.slot_stride * 2) + ((p ^ (values ? TR::swizzle_v(r) : TR::swizzle(r))) << 4);
+    }
+    const auto load_lds = [](uint32_t off, const char *src, uint32_t dst) __attribute__((always_inline)) {
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(src), "s"(dst) : "memory", "m0");
+    };
+    const auto wait_loads = [](auto newer) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(newer)::value) : "memory");
+    };
+    const auto meet = []() __attribute__((always_inline)) {   // what the wave reads and writes in LDS is done
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // K^T Q: a lane reads key n31, channels 8 half .. + 7 of 16; V^T P: four keys of a channel, lanes of a sixteen the channels, keys 4 half .. + 3 and 8 behind them
+    const uint32_t k_read = n31 * ROWB + ((half ^ TR::swizzle(n31)) << 4);
+    uint32_t v_read[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const int r = 8 * x + 4 * half + ((lane & 15) >> 2);
+        v_read[x] = TR::kValues + r * ROWB + (((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ TR::swizzle_v(r)) << 4) + (lane & 1) * 8;
+    }
+    const uint32_t *row_mask = reinterpret_cast<const uint32_t *>(lds + TR::kMask);
+    const int *row_begin = reinterpret_cast<const int *>(lds + TR::kBegin);
+    uint32_t *flags = reinterpret_cast<uint32_t *>(lds + TR::kThere), *bad = reinterpret_cast<uint32_t *>(lds + TR::kBad);
+    const float c = a.cap_log2e > 0.f ? a.cap_log2e : a.scale_log2e;
+
+    Place at = range.at;
+    int pos = range.begin;
+    Seq seq = seq_of<KEYS, ROWS>(a, at.seq, ScalarLoad{});
+    while (pos < range.end) {
+        while (at.item == seq.items) {   // the next sequence that has some
+            at.item = 0;
+            seq = seq_of<KEYS, ROWS>(a, ++at.seq, ScalarLoad{});
+        }
+        const int block = max(0, at.unit - kItemBlocks);   // the first one
+        const int n_steps = min(seq.blocks - block, range.end - pos - max(0, kItemBlocks - at.unit));
+        if (n_steps <= 0) break;   // the share ends where the item begins
+        const int kvh = at.item / seq.groups, row0 = (at.item - kvh * seq.groups) * ROWS;   // rows: token by token, the group's heads of each
+        const int n_rows = min(ROWS, seq.T * a.G - row0);
+        const int b0 = seq.first + block;
+
+        // The wave's 16 slots of the next blocks that it requests (a page holds P16 such), and the place in the ring that they go to
+        const int32_t *table = a.cache.page_table + (int64_t)at.seq * a.cache.max_pages;
+        const char *head = pool + (int64_t)kvh * a.cache.head_stride * 2;
+        int page = (b0 * 2 + sub) / P16, in16 = b0 * 2 + sub - page * P16, to = 0;
+        const auto page_number = [&]() __attribute__((always_inline)) { return page < a.cache.max_pages ? scalar_load<int>(table + page) : -1; };
+        const auto go_on = [&]() __attribute__((always_inline)) {
+            in16 += 2;
+            const int on = in16 < P16 ? 0 : P16 == 1 ? 2 : 1;   // pages
+            in16 -= on * P16;
+            page += on;
+        };
+        const auto issue = [&](int number, int in16) __attribute__((always_inline)) {
+            const bool ok = (uint32_t)number < (uint32_t)a.cache.n_pages;
+            const char *src = head + (ok ? number : 0) * page_bytes + in16 * slots16_bytes;
+#pragma unroll
+            for (int x = 0; x < NI16; ++x) load_lds(voff[x], src, to0 + to * BLK + x * 1024);
+            if (lane == 0) (values ? bad : flags)[values ? to : to * 2 + sub] = ok && !values ? 0xffffu : 0u;
+            to = to + 1 == RING ? 0 : to + 1;
+        };
+        int next_page = 0;   // of the block to be requested next
+        const auto issue_first = [&](int n) __attribute__((always_inline)) {   // up to RING - 1 or RING blocks: their page numbers come together
+            int number[RING], at16[RING];
+#pragma unroll
+            for (int r = 0; r < RING; ++r) {
+                number[r] = r < n ? page_number() : 0;
+                at16[r] = in16;
+                if (r < n) go_on();
+            }
+            next_page = page_number();
+#pragma unroll
+            for (int r = 0; r < RING; ++r)
+                if (r < n) issue(number[r], at16[r]);
+        };
+
+        // Two waves request the first keys, the others the query rows and what they see, in the layout of a K block and where values go later.  A place without a row holds a copy of the last
+        // one.
+        if (!values) {
+            issue_first(min(RING, n_steps));
+            if (n_steps < RING) wait_loads(std::integral_constant<int, 0>{});
+            else wait_loads(std::integral_constant<int, (RING - 1) * NI16>{});
+        } else {
+            const char *qh = reinterpret_cast<const char *>(static_cast<const __bf16 *>(a.q) + seq.token * a.q_token + (int64_t)kvh * a.G * a.q_head);
+            constexpr int kAll = ROWS * ROWB / 1024;
+            int l = lane;
+            asm volatile("" : "+v"(l));   // (else what depends on the lane alone is kept in registers over all items)
+#pragma unroll
+            for (int i0 = 0; i0 < kAll; i0 += 2) {
+                const int i = i0 + sub, r = i * (1024 / ROWB) + l / (ROWB / 16), p = l % (ROWB / 16);
+                const int R = row0 + min(r, n_rows - 1), t = token_of(a, R);
+                load_lds((uint32_t)((t * a.q_token + (R - t * a.G) * a.q_head) * 2) + ((p ^ TR::swizzle(r)) << 4), qh, lds0 + TR::kValues + i * 1024);
+            }
+            rows_see<ROWS, 128>(a, seq, row0, n_rows, reinterpret_cast<uint32_t *>(lds + TR::kMask), reinterpret_cast<int *>(lds + TR::kBegin), tid - 128);
+            wait_loads(std::integral_constant<int, 0>{});
+        }
+        meet();   // the first block's keys, the query rows and what they see are there
+        bf16x8 q[KSTEPS];
+#pragma unroll
+        for (int t = 0; t < KSTEPS; ++t) q[t] = *reinterpret_cast<const bf16x8 *>(lds + TR::kValues + wave * 32 * ROWB + (k_read ^ (t << 5)));
+        meet();   // all query rows are in registers
+        if (values) issue_first(min(RING - 1, n_steps));
+
+        floatx16 o[CB], s;
+        float m_run = -INFINITY, l_run = 0.f;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[cb][i] = 0.f;
+        // Slots below this one, if their pages are there, are seen by all rows, but for those before the window's last begin.
+        const int window_end = a.window > 0 ? min(seq.base, seq.base - a.window + seq.T) : 0;
+        const bool works = wave * 32 < n_rows;
+
+        // ---- S^T = K Q^T of the block at `from`: lane: row n31, slots 8 b + 4 half + e in [4 b + e]
+        const auto scores = [&](int from) __attribute__((always_inline)) {
+            floatx16 x;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = 0.f;
+#pragma unroll
+            for (int t = 0; t < KSTEPS; ++t) {
+                const bf16x8 f = *reinterpret_cast<const bf16x8 *>(lds + ((k_read + from * BLK) ^ (t << 5)));
+                x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[t], x, 0, 0, 0);
+            }
+            return x;
+        };
+        // ---- which slots of a block may be looked at, and whether that, or what a row may see, is less than all.  Blocks whole_from .. whole_to - 1 are whole if
+        // their pages are there.
+        const int whole_from = (max(window_end, seq.begin) + KEYS - 1) / KEYS - b0, whole_to = seq.base / KEYS - b0;
+        uint32_t exists = ~0u;
+        bool masked = false;
+        const auto look = [&](int i, uint2 pages) __attribute__((always_inline)) {
+            exists = __builtin_amdgcn_readfirstlane(pages.x | pages.y << 16);
+            masked = i < whole_from || i >= whole_to || exists != ~0u;
+            if (masked) {
+                const int n0 = (b0 + i) * KEYS;
+                if (n0 < seq.begin) exists &= ~0u << min(31, seq.begin - n0);   // (a block has a visible slot: seq.begin - n0 < KEYS)
+                if (n0 + KEYS > seq.n) exists &= n0 < seq.n ? ~(~0u << (seq.n - n0)) : 0u;
+            }
+        };
+        // ---- the largest score of a lane's slots
+        const auto largest = [](const floatx16 &x) __attribute__((always_inline)) {
+            float m[5];
+#pragma unroll
+            for (int e = 0; e < 5; ++e) m[e] = fmaxf(fmaxf(x[3 * e], x[3 * e + 1]), x[3 * e + 2]);
+            return fmaxf(fmaxf(fmaxf(fmaxf(m[0], m[1]), m[2]), fmaxf(fmaxf(m[3], m[4]), x[15])), -INFINITY);
+        };
+        // ---- what the lane's row sees of it, and the row's reference point (see tree_shares); l and O follow it.  mx: of the scores as they come
+        uint32_t seen = 0;
+        const auto refer = [&](int i, float mx) __attribute__((always_inline)) {
+            if (a.cap_log2e > 0.f) {
+                floatx16 x[1] = {s};
+                tanh_scores(x, a.to_cap);
+                s = x[0];
+            }
+            if (masked) {
+                seen = (row_sees<ROWS>(row_mask, row_begin, wave * 32 + n31, (b0 + i) * KEYS, seq.base) & exists) >> (4 * half);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = (seen & (1u << (8 * (e / 4) + e % 4))) ? s[e] : -INFINITY;
+            }
+            if (masked || a.cap_log2e > 0.f) mx = largest(s);
+            mx = max_across_halves(mx);
+            const bool grow = fmaf(mx, c, -(m_run * c)) > 8.f;
+            if (__any(grow)) {
+                const float m_new = grow ? mx : m_run;
+                const float alpha = grow ? __builtin_amdgcn_exp2f((m_run - m_new) * c) : 1.f;   // (m_new is a number where it grew)
+                l_run *= alpha;
+                m_run = m_new;
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[cb][e] *= alpha;
+            }
+        };
+
+        int from = 0;   // place of this block in the rings
+        const uint2 *pages = reinterpret_cast<const uint2 *>(flags);
+        look(0, pages[0]);   // (the first keys and their flags are there: all waves have waited for them)
+        if (works) {
+            s = scores(0);
+            refer(0, largest(s));
+        }
+        for (int i = 0; i < n_steps; ++i) {
+            if (i + RING - 1 < n_steps) wait_loads(std::integral_constant<int, (RING - 2) * NI16>{});
+            else wait_loads(std::integral_constant<int, 0>{});
+            meet();   // the next keys, this block's values are there; this block's keys and the values before are free
+            if (i + RING - (values ? 1 : 0) < n_steps) {
+                issue(next_page, in16);
+                go_on();
+                next_page = page_number();
+            }
+            const int next = from + 1 == RING ? 0 : from + 1;
+            const uint2 next_pages = pages[next];
+            float next_mx = 0.f;
+            // Values in a masked block: those that nobody may look at, and any infinity or NaN, are replaced by zero; times a probability of zero they would be a NaN.
+            // Rows that do see such a slot get one through their sum.
+            if (masked) {
+                for (int x = tid; x < BLK / 16; x += THREADS) {
+                    const int r = x / (ROWB / 16);
+                    uint4 *v = reinterpret_cast<uint4 *>(lds + TR::kValues + from * BLK) + x;
+                    const uint4 y = *v;
+                    const uint32_t z[4] = {y.x, y.y, y.z, y.w};
+                    bool finite = true;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) finite = finite && (z[w] & 0x7f80u) != 0x7f80u && (z[w] & 0x7f800000u) != 0x7f800000u;
+                    if (!finite || !(exists >> r & 1)) *v = make_uint4(0, 0, 0, 0);
+                    if (!finite && (exists >> r & 1)) atomicOr(bad + from, 1u << r);
+                }
+                meet();
+                if (works && (seen & bad[from] >> (4 * half))) l_run = __builtin_nanf("");
+            }
+            if (works) {
+                const auto read_v = [&](int j, int cb) __attribute__((always_inline)) {   // channel 32 cb + n31, slots 16 j + 4 half .. + 3 and 8 behind them
+                    const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(lds + ((v_read[0] + from * BLK) ^ (cb << 6)) + j * 16 * ROWB)));
+                    const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(lds + ((v_read[1] + from * BLK) ^ (cb << 6)) + j * 16 * ROWB)));
+                    return __builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, y.x, y.y));
+                };
+                // the next block's scores (behind the last one: of whatever is there) beside this one's probabilities
+                bf16x8 vf[2][CB];
+#pragma unroll
+                for (int j = 0; j < 1; ++j)
+#pragma unroll
+                    for (int cb = 0; cb < CB; ++cb) vf[j][cb] = read_v(j, cb);
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(1);
+                const floatx16 s_next = scores(next);
+                const float off = m_run == -INFINITY ? 0.f : -(m_run * c);   // no slot so far: p = 0
+                float sum[2] = {0.f, 0.f};
+                bf16x8 pb[2], rest[2];   // of 16 slots each, as two numbers (see tree_shares)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    floatx8 x;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        x[e] = __builtin_amdgcn_exp2f(fmaf(s[8 * j + e], c, off));
+                        sum[e & 1] += x[e];
+                    }
+                    pb[j] = __builtin_convertvector(x, bf16x8);
+                    rest[j] = __builtin_convertvector(x - __builtin_convertvector(pb[j], floatx8), bf16x8);
+                }
+                l_run += sum[0] + sum[1];
+                // ---- O^T += V^T P^T
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int cb = 0; cb < CB; ++cb) {
+                        const bf16x8 f = j == 0 ? vf[0][cb] : read_v(j, cb);
+                        o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pb[j], o[cb], 0, 0, 0);
+                        o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, rest[j], o[cb], 0, 0, 0);
+                    }
+                __builtin_amdgcn_s_setprio(0);
+                s = s_next;
+                next_mx = largest(s);
+            }
+            if (i + 1 < n_steps) {
+                look(i + 1, next_pages);
+                if (works) refer(i + 1, next_mx);
+            }
+            from = next;
+        }
+
+        // ---- results over the rings; [row][chunks of 4 channels, exchanged]
+        meet();   // all waves have read their last block
+        float2 *ml = reinterpret_cast<float2 *>(lds + TR::kMl);
+        float4 *merge = reinterpret_cast<float4 *>(lds);
+        if (works) {
+            const int row = wave * 32 + n31;
+            const float l = sum_across_halves(l_run);
+            if (half == 0) ml[row] = make_float2(m_run, l);
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                for (int b = 0; b < 4; ++b)   // channels 32 cb + 8 b + 4 half + i
+                    merge[row * CH4 + ((8 * cb + 2 * b + half) ^ (row & (CH4 - 1)))] = make_float4(o[cb][4 * b], o[cb][4 * b + 1], o[cb][4 * b + 2], o[cb][4 * b + 3]);
+        }
+        __syncthreads();
+        const bool begins = block == 0, ends = block + n_steps == seq.blocks;
+        const int64_t into = (int64_t)(2 * blockIdx.x + (begins ? 1 : 0)) * ROWS;
+        for (int idx = tid; idx < n_rows * CH4; idx += THREADS) {
+            const int row = idx / CH4, ch = idx % CH4;
+            const float2 x = ml[row];
+            const float4 y = merge[row * CH4 + (ch ^ (row & (CH4 - 1)))];
+            if (begins && ends) {
+                const float inv = x.y == 0.f ? 0.f : 1.f / x.y;
+                const int R = row0 + row, t = token_of(a, R);
+                store_row4(static_cast<__bf16 *>(a.out) + (seq.token + t) * a.out_token + (int64_t)(kvh * a.G + R - t * a.G) * a.out_head + 4 * ch,
+                           make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv));
+            } else {
+                *reinterpret_cast<float4 *>(a.part_o + (into + row) * D + 4 * ch) = y;
+                if (ch == 0) a.part_ml[into + row] = x;
             }
         }
         if (begins && tid == 0 && (a.by_item || !ends))
@@ -695,7 +1079,7 @@ __global__ __launch_bounds__(256) void tree_join(const TreeArgs a)
     const Seq seq = seq_of<sizeof(T) == 2 ? 32 : 16, M>(a, cut.seq, VectorLoad{});
     const int kvh = cut.item / seq.groups, row0 = (cut.item - kvh * seq.groups) * M;
     if (row >= min(M, seq.T * a.G - row0)) return;
-    const float c = a.cap_log2e > 0.f ? 1.f : a.scale_log2e;
+    const float c = a.cap_log2e > 0.f ? a.cap_log2e : a.scale_log2e;
     float m = -INFINITY, l = 0.f;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     // loads of eight parts go out together ; those behind the last one to that one
@@ -740,7 +1124,7 @@ __global__ __launch_bounds__(256) void tree_join(const TreeArgs a)
         sum.x = fmaf(y.x, g, sum.x); sum.y = fmaf(y.y, g, sum.y); sum.z = fmaf(y.z, g, sum.z); sum.w = fmaf(y.w, g, sum.w);
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int R = row0 + row, t = R / a.G;
+    const int R = row0 + row, t = token_of(a, R);
     store_row4(static_cast<T *>(a.out) + (seq.token + t) * a.out_token + (int64_t)(kvh * a.G + R - t * a.G) * a.out_head + 4 * ch,
                make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
 }
@@ -751,41 +1135,62 @@ constexpr int kMaxDevices = 64;
 std::mutex g_mutex;
 int g_n_cus[kMaxDevices];   // compute units of a device, once its kernels' limits are raised
 
-// The kernel for up to M rows of a sequence and KV head: f(NRB, WR, WK as types).  fp32: 256 rows of queries would not fit beside the ring, nor would four
-// rings beside 64.
-template <typename T, typename F>
+template <typename T, int D, int NRB, int WR, int WK>
+struct Narrow {
+    typedef Layout<T, D, NRB, WR, WK> layout;
+    static constexpr auto kernel = tree_shares<T, D, NRB, WR, WK>;
+};
+template <int D>
+struct Broad {
+    typedef Wide<D> layout;
+    static constexpr auto kernel = tree_wide<D>;
+};
+
+// The kernel for up to M rows of a sequence and KV head: f(its type).
+template <typename T, int D, typename F>
 auto with_rows(int32_t M, F f)
 {
-    using std::integral_constant;
-    typedef integral_constant<int, 1> one;
-    typedef integral_constant<int, 2> two;
-    typedef integral_constant<int, 4> four;
-    typedef integral_constant<int, 8> eight;
-    switch (M) {
-    case 16: return f(one{}, one{}, four{});
-    case 32: return f(two{}, one{}, four{});
-    case 64:
-        if constexpr (sizeof(T) == 2) return f(two{}, two{}, four{});
-        else return f(two{}, two{}, two{});
-    case 128: return f(two{}, four{}, two{});
-    default:
-        if constexpr (sizeof(T) == 2) return f(two{}, eight{}, one{});
-        else return f(two{}, four{}, two{});
+    if constexpr (sizeof(T) == 2) {
+        switch (M) {
+        case 16: return f(Narrow<T, D, 1, 1, 4>{});
+        case 32: return f(Narrow<T, D, 2, 1, 4>{});
+        default: return f(Broad<D>{});
+        }
+    } else {   // (more rows, or more rings beside 64, do not fit the LDS)
+        switch (M) {
+        case 16: return f(Narrow<T, D, 1, 1, 4>{});
+        case 32: return f(Narrow<T, D, 2, 1, 4>{});
+        case 64: return f(Narrow<T, D, 2, 2, 2>{});
+        default: return f(Narrow<T, D, 2, 4, 2>{});
+        }
     }
 }
 
 int32_t rows_of(int64_t rows, int32_t dtype)
 {
-    return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 || dtype == BS_F32 ? 128 : 256;
+    if (rows <= 32) return rows <= 16 ? 16 : 32;
+    return dtype == BS_F32 ? (rows <= 64 ? 64 : 128) : 128;
+}
+
+// What the host has to know of the kernel's layout.
+struct Traits { int32_t keys, per_cu, turns; };
+Traits traits_of(const bs_cache &c, int32_t M)
+{
+    const auto get = [](auto k) {
+        typedef typename decltype(k)::layout L;
+        return Traits{L::kKeys, L::kPerCu, L::kTurns};
+    };
+    if (c.dtype == BS_BF16) return c.head_dim == 64 ? with_rows<__bf16, 64>(M, get) : with_rows<__bf16, 128>(M, get);
+    return c.head_dim == 64 ? with_rows<float, 64>(M, get) : with_rows<float, 128>(M, get);
 }
 
 template <typename T, int D>
 hipError_t raise_limits()
 {
-    for (int M : {16, 32, 64, 128, 256}) {
-        const hipError_t e = with_rows<T>(M, [](auto nrb, auto wr, auto wk) {
-            constexpr int NRB = decltype(nrb)::value, WR = decltype(wr)::value, WK = decltype(wk)::value;
-            return hipFuncSetAttribute(reinterpret_cast<const void *>(tree_shares<T, D, NRB, WR, WK>), hipFuncAttributeMaxDynamicSharedMemorySize, Layout<T, D, NRB, WR, WK>::kLds);
+    for (int M : {16, 32, 64, 128}) {
+        const hipError_t e = with_rows<T, D>(M, [](auto k) {
+            typedef decltype(k) K;
+            return hipFuncSetAttribute(reinterpret_cast<const void *>(K::kernel), hipFuncAttributeMaxDynamicSharedMemorySize, K::layout::kLds);
         });
         if (e != hipSuccess) return e;
     }
@@ -830,15 +1235,15 @@ struct Plan {
 
 int make_plan(const bs_cache &c, int32_t n_q_heads, int32_t n_tokens, int32_t max_tokens, int n_cus, Plan *p)
 {
-    const int32_t G = n_q_heads / c.n_kv_heads, keys = c.dtype == BS_BF16 ? 32 : 16;
+    const int32_t G = n_q_heads / c.n_kv_heads;
     const int64_t rows = (int64_t)G * std::min(std::max(1, n_tokens), max_tokens);   // of a sequence and KV head
-    if (rows > 1 << 24) return BS_EUNSUPPORTED;
+    if (rows > 1 << 20) return BS_EUNSUPPORTED;   // (see token_of)
     p->M = rows_of(rows, c.dtype);
-    const int64_t groups = (rows + p->M - 1) / p->M, per_item = (cache_slots(c) + keys - 1) / keys + 1, items = (int64_t)c.n_seqs * c.n_kv_heads;
+    const Traits t = traits_of(c, p->M);
+    const int64_t groups = (rows + p->M - 1) / p->M, per_item = (cache_slots(c) + t.keys - 1) / t.keys + 1, items = (int64_t)c.n_seqs * c.n_kv_heads;
     if (items > INT32_MAX / groups || items * groups > INT32_MAX / 2 / (per_item + kItemBlocks)) return BS_EUNSUPPORTED;   // units are counted in 32 bits
     p->most_items = (int32_t)(groups * c.n_kv_heads);
-    const int per_cu = c.head_dim == 64 && p->M <= 32 ? 2 : 1, turns = p->M <= (c.dtype == BS_BF16 ? 64 : 32) ? 4 : p->M <= 128 ? 2 : 1;   // (see Layout)
-    p->n_shares = (int32_t)std::min<int64_t>((int64_t)n_cus * per_cu, (items * groups * per_item + turns - 1) / turns);
+    p->n_shares = (int32_t)std::min<int64_t>((int64_t)n_cus * t.per_cu, (items * groups * per_item + t.turns - 1) / t.turns);
     const auto whole = [](int64_t bytes) { return (bytes + 255) / 256 * 256; };
     p->part_o = 0;
     p->part_ml = whole((int64_t)2 * p->n_shares * p->M * c.head_dim * 4);
@@ -851,10 +1256,10 @@ int make_plan(const bs_cache &c, int32_t n_q_heads, int32_t n_tokens, int32_t ma
 template <typename T, int D>
 int launch(const TreeArgs &a, const Plan &p, hipStream_t st)
 {
-    return with_rows<T>(p.M, [&](auto nrb, auto wr, auto wk) {
-        constexpr int NRB = decltype(nrb)::value, WR = decltype(wr)::value, WK = decltype(wk)::value;
-        using L = Layout<T, D, NRB, WR, WK>;
-        hipError_t e = launch_kernel(tree_shares<T, D, NRB, WR, WK>, dim3((unsigned)p.n_shares), dim3(L::kThreads), L::kLds, st, a);
+    return with_rows<T, D>(p.M, [&](auto k) {
+        typedef decltype(k) K;
+        typedef typename K::layout L;
+        hipError_t e = launch_kernel(K::kernel, dim3((unsigned)p.n_shares), dim3(L::kThreads), L::kLds, st, a);
         if (e != hipSuccess) return fail_hip(e, "tree_shares launch");
         if (p.n_shares > 1) e = launch_kernel(tree_join<T, D, L::kRows>, dim3((unsigned)p.n_cuts, (unsigned)L::kRows), dim3(256), 0, st, a);
         return e == hipSuccess ? BS_OK : fail_hip(e, "tree_join launch");
@@ -909,6 +1314,7 @@ extern "C" int bs_attn_tree(const bs_cache *cache, const bs_heads *q, const bs_h
     a.n_tokens = n_tokens;
     a.max_tokens = std::min(n_tokens, max_tokens);
     a.G = G;
+    a.inv_g = 1.f / G;
     a.window = window;
     a.most_items = p.most_items;
     a.scale_log2e = scale * 1.4426950408889634f;
