@@ -49,6 +49,7 @@ struct TreeArgs {
 template <typename T, int D, int NRB, int WR, int WK>
 struct Layout {
     static constexpr int kWaves = WR * WK, kThreads = 64 * kWaves, kRows = 16 * NRB * WR, kTurns = WK;
+    static constexpr int kItem = 8;                           // beginning an item costs about as much as so many blocks: shares are equal with that counted
     static constexpr int kKeys = sizeof(T) == 2 ? 32 : 16;    // slots of a block
     static constexpr int kRowBytes = D * (int)sizeof(T);
     static constexpr int kBlock = kKeys * kRowBytes;          // one block of K or V
@@ -60,9 +61,7 @@ struct Layout {
     static constexpr int kQuery = WK * kGroup;                // the query rows behind the rings
     static constexpr int kMerge = WR > 1 ? kRows * D * 4 : kGroup;   // a group's results lie over the ring; where its waves have it alone, over its own part
     static constexpr int kEnd = kQuery + kRows * kRowBytes > WK * kMerge ? kQuery + kRows * kRowBytes : WK * kMerge;
-    static constexpr int kMask = kEnd;                        // [8][rows]: bits of the drafted tokens
-    static constexpr int kBegin = kMask + 8 * kRows * 4;      // [rows]: first slot seen
-    static constexpr int kMl = kBegin + kRows * 4;            // [groups][rows]
+    static constexpr int kMl = kEnd;                          // [groups][rows]
     static constexpr int kLds = kMl + WK * kRows * 8;
     static constexpr int kPerCu = D == 64 && WR == 1 ? 2 : 1; // workgroups per CU
     static_assert((kLds + 1024) * kPerCu <= 160 * 1024, "LDS of a CU");   // (with what own_range has)
@@ -71,15 +70,13 @@ struct Layout {
     __device__ static int swizzle(int r) { return kRowBytes == 128 ? (r >> 1) & 7 : r & 15; }
 };
 
-// Beginning an item costs about as much as so many blocks: shares are equal with that counted.
-constexpr int kItemBlocks = 4;
 
 typedef float floatx8 __attribute__((ext_vector_type(8)));
 
 // A sequence: slots in use, its drafted tokens; what is visible of it, from block `first` on; units: of an item, with its beginning; items of it.
 struct Seq { int base, token, T, n, begin, first, blocks, units, groups, items; };
 
-template <int KEYS, int M, typename LOAD>
+template <typename L, typename LOAD>
 __device__ inline Seq seq_of(const TreeArgs &a, int s, LOAD load)
 {
     Seq v;
@@ -89,11 +86,11 @@ __device__ inline Seq seq_of(const TreeArgs &a, int s, LOAD load)
     v.T = min(max(v.token, min(load(a.first + s + 1), a.n_tokens)) - v.token, a.max_tokens);
     v.n = min(v.base + v.T, cap);
     v.begin = a.window > 0 ? max(0, v.base - a.window) : 0;
-    v.first = v.begin / KEYS;
-    v.blocks = (v.n + KEYS - 1) / KEYS - v.first;
-    v.groups = (v.T * a.G + M - 1) / M;
+    v.first = v.begin / L::kKeys;
+    v.blocks = (v.n + L::kKeys - 1) / L::kKeys - v.first;
+    v.groups = (v.T * a.G + L::kRows - 1) / L::kRows;
     v.items = v.groups * a.cache.n_kv_heads;
-    v.units = v.T > 0 ? v.blocks + kItemBlocks : 0;
+    v.units = v.T > 0 ? v.blocks + L::kItem : 0;
     return v;
 }
 // Row R of a sequence and KV head is token R / G.  (R + 1/2) / G is at least 1 / (2 G) away from whole numbers, and off by less than that for R below 2^21.
@@ -107,16 +104,16 @@ struct Place { int seq, item, unit; };   // sequence, item of it, unit of that
 struct Range { int begin, end; Place at; int each; };   // `each`: units of a share
 
 // All threads of the workgroup; units of a share: a multiple of the groups of waves.
-template <int KEYS, int M, int WK, int THREADS>
+template <typename L>
 __device__ inline Range own_range(const TreeArgs &a, int share, int n_shares)
 {
-    constexpr int kWaves = THREADS / 64;
+    constexpr int THREADS = L::kThreads, kWaves = THREADS / 64, WK = L::kTurns;
     __shared__ int wave_sums[kWaves], found[3];
     const int tid = threadIdx.x, S = a.cache.n_seqs;
     Range r;
     int total;
     if (S == 1) {
-        const Seq v = seq_of<KEYS, M>(a, 0, ScalarLoad{});
+        const Seq v = seq_of<L>(a, 0, ScalarLoad{});
         total = v.units * v.items;
         r.each = max(WK, ((total + n_shares - 1) / n_shares + WK - 1) / WK * WK);
         r.begin = (int)min((int64_t)total, (int64_t)share * r.each);
@@ -130,7 +127,7 @@ __device__ inline Range own_range(const TreeArgs &a, int share, int n_shares)
     const int each = (S + THREADS - 1) / THREADS, s0 = min(S, tid * each), s1 = min(S, s0 + each);
     int mine = 0;
     for (int s = s0; s < s1; ++s) {
-        const Seq v = seq_of<KEYS, M>(a, s, VectorLoad{});
+        const Seq v = seq_of<L>(a, s, VectorLoad{});
         mine += v.units * v.items;
     }
     int upto = mine;
@@ -153,10 +150,10 @@ __device__ inline Range own_range(const TreeArgs &a, int share, int n_shares)
     r.end = min(total, r.begin + r.each);
     if (r.begin >= before && r.begin < before + mine) {
         int left = r.begin - before, s = s0;
-        Seq v = seq_of<KEYS, M>(a, s, VectorLoad{});
+        Seq v = seq_of<L>(a, s, VectorLoad{});
         while (left >= v.units * v.items) {
             left -= v.units * v.items;
-            v = seq_of<KEYS, M>(a, ++s, VectorLoad{});
+            v = seq_of<L>(a, ++s, VectorLoad{});
         }
         found[0] = s;
         found[1] = left / v.units;
@@ -205,53 +202,58 @@ __device__ inline void tanh_scores(V (&s)[N], float to_cap)
         }
 }
 
-// What the rows of an item see of the drafted tokens, [8 words][ROWS], and where a window begins, [ROWS], into LDS.  Threads tid of THREADS.
+// What drafted token t of a sequence sees of the drafted ones, with the window laid on; returns the first slot that it sees.
+__device__ inline int token_sees(const TreeArgs &a, const Seq &seq, int t, uint64_t (&words)[BS_TREE_MAX_TOKENS / 64])
+{
+    int seen = 0;
+#pragma unroll
+    for (int w = 0; w < BS_TREE_MAX_TOKENS / 64; ++w) {
+        uint64_t x = a.mask ? 0 : bits_between(0, t + 1 - 64 * w);
+        if (a.mask && w < a.mask_words) x = a.mask[(int64_t)(seq.token + t) * a.mask_words + w];
+        words[w] = x;
+    }
+#pragma unroll
+    for (int w = 0; w < BS_TREE_MAX_TOKENS / 64; ++w) {
+        words[w] &= bits_between(0, seq.T - 64 * w);
+        seen += __popcll(words[w]);
+    }
+    if (a.window <= 0) return 0;
+    int drop = seen - a.window;   // the first ones
+#pragma unroll
+    for (int w = 0; w < BS_TREE_MAX_TOKENS / 64; ++w) {
+        const int n = __popcll(words[w]);
+        if (drop >= n) words[w] = 0;
+        else for (int i = 0; i < drop; ++i) words[w] &= words[w] - 1;
+        drop -= n;
+    }
+    return max(0, seq.base - max(0, a.window - seen));
+}
+
+// The same of the rows of an item, [8 words][ROWS] and [ROWS], into LDS.  Threads tid of THREADS.
 template <int ROWS, int THREADS>
 __device__ inline void rows_see(const TreeArgs &a, const Seq &seq, int row0, int n_rows, uint32_t *masks, int *begins, int tid)
 {
     for (int r = tid; r < ROWS; r += THREADS) {
-        const int t = token_of(a, row0 + min(r, n_rows - 1));
         uint64_t words[BS_TREE_MAX_TOKENS / 64];
-        int seen = 0;
-#pragma unroll
-        for (int w = 0; w < BS_TREE_MAX_TOKENS / 64; ++w) {
-            uint64_t x = a.mask ? 0 : bits_between(0, t + 1 - 64 * w);
-            if (a.mask && w < a.mask_words) x = a.mask[(int64_t)(seq.token + t) * a.mask_words + w];
-            words[w] = x & bits_between(0, seq.T - 64 * w);
-            seen += __popcll(words[w]);
-        }
-        int begin = 0;
-        if (a.window > 0) {
-            begin = max(0, seq.base - max(0, a.window - seen));
-            int drop = seen - a.window;   // the first ones
-#pragma unroll
-            for (int w = 0; w < BS_TREE_MAX_TOKENS / 64; ++w) {
-                const int n = __popcll(words[w]);
-                if (drop >= n) words[w] = 0;
-                else for (int i = 0; i < drop; ++i) words[w] &= words[w] - 1;
-                drop -= n;
-            }
-        }
+        begins[r] = token_sees(a, seq, token_of(a, row0 + min(r, n_rows - 1)), words);
 #pragma unroll
         for (int w = 0; w < 8; ++w) masks[w * ROWS + r] = (uint32_t)(words[w / 2] >> (32 * (w % 2)));
-        begins[r] = begin;
     }
 }
 
-// 32 slots from n0 on that a row sees.
-template <int ROWS>
-__device__ inline uint32_t row_sees(const uint32_t *masks, const int *begins, int row, int n0, int base)
+// 32 slots from n0 on that a row sees; word(w): 32 drafted tokens; begin: first slot seen.
+template <typename W>
+__device__ inline uint32_t row_sees(int n0, int base, int begin, W word)
 {
     const int rel = n0 - base;   // drafted token of the first slot
     uint32_t x;
     if (rel >= 0) {
         const int w = min(rel >> 5, 8);
-        const uint32_t lo = w < 8 ? masks[w * ROWS + row] : 0, hi = w < 7 ? masks[(w + 1) * ROWS + row] : 0;
-        x = __builtin_amdgcn_alignbit(hi, lo, rel & 31);
+        x = __builtin_amdgcn_alignbit(w < 7 ? word(w + 1) : 0u, w < 8 ? word(w) : 0u, rel & 31);
     } else {
-        x = rel > -32 ? (masks[row] << (-rel & 31)) | ~(~0u << (-rel & 31)) : ~0u;
+        x = rel > -32 ? (word(0) << (-rel & 31)) | ~(~0u << (-rel & 31)) : ~0u;
     }
-    const int before = begins[row] - n0;   // slots that lie before the row's window
+    const int before = begin - n0;   // slots that lie before the row's window
     if (before > 0) x &= before < 32 ? ~0u << before : 0u;
     return x;
 }
@@ -271,9 +273,9 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
     // items that a sequence could have and has not: nothing to join
     if (a.by_item)
         for (int s = blockIdx.x; s < a.cache.n_seqs; s += gridDim.x)
-            for (int i = seq_of<KEYS, ROWS>(a, s, ScalarLoad{}).items + tid; i < a.most_items; i += THREADS) a.cuts[s * a.most_items + i] = Cut{s, i, 0, 0};
+            for (int i = seq_of<TR>(a, s, ScalarLoad{}).items + tid; i < a.most_items; i += THREADS) a.cuts[s * a.most_items + i] = Cut{s, i, 0, 0};
 
-    const Range range = own_range<KEYS, ROWS, WK, THREADS>(a, blockIdx.x, gridDim.x);
+    const Range range = own_range<TR>(a, blockIdx.x, gridDim.x);
     if (tid == 0 && !a.by_item) a.cuts[blockIdx.x] = Cut{0, -1, 0, 0};
     if (range.begin >= range.end) return;
 
@@ -315,19 +317,17 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
             v_read[i] = wk * TR::kGroup + BLK + r * ROWB + ((col ^ TR::swizzle(r)) << 4);
         }
     }
-    const uint32_t *row_mask = reinterpret_cast<const uint32_t *>(lds + TR::kMask);
-    const int *row_begin = reinterpret_cast<const int *>(lds + TR::kBegin);
 
     Place at = range.at;
     int pos = range.begin;
-    Seq seq = seq_of<KEYS, ROWS>(a, at.seq, ScalarLoad{});
+    Seq seq = seq_of<TR>(a, at.seq, ScalarLoad{});
     while (pos < range.end) {
         while (at.item == seq.items) {   // the next sequence that has some
             at.item = 0;
-            seq = seq_of<KEYS, ROWS>(a, ++at.seq, ScalarLoad{});
+            seq = seq_of<TR>(a, ++at.seq, ScalarLoad{});
         }
-        const int block = max(0, at.unit - kItemBlocks);   // the first one
-        const int blocks = min(seq.blocks - block, range.end - pos - max(0, kItemBlocks - at.unit));
+        const int block = max(0, at.unit - TR::kItem);   // the first one
+        const int blocks = min(seq.blocks - block, range.end - pos - max(0, TR::kItem - at.unit));
         if (blocks <= 0) break;   // the share ends where the item begins
         const int kvh = at.item / seq.groups, row0 = (at.item - kvh * seq.groups) * ROWS;   // rows: token by token, the group's heads of each
         const int n_rows = min(ROWS, seq.T * a.G - row0);
@@ -401,7 +401,6 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
                 issue(s1.v, ring + 3 * BLK);
             }
         }
-        rows_see<ROWS, THREADS>(a, seq, row0, n_rows, reinterpret_cast<uint32_t *>(lds + TR::kMask), reinterpret_cast<int *>(lds + TR::kBegin), tid);
         if (!SHARED && n_steps > 1) wait_loads(std::integral_constant<int, 4 * NI>{});
         else if (!SHARED && n_steps == 1) wait_loads(std::integral_constant<int, 2 * NI>{});
         else wait_loads(std::integral_constant<int, 0>{});
@@ -505,7 +504,16 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
             if (masked) {
 #pragma unroll
                 for (int rb = 0; rb < NRB; ++rb) {
-                    const uint32_t x = row_sees<ROWS>(row_mask, row_begin, (wr * NRB + rb) * 16 + col, n0, seq.base);
+                    // (one or two blocks of an item: loaded when it comes to them, not when the item begins and its first keys are under way)
+                    uint32_t x = ~0u;
+                    if (n0 + KEYS > seq.base || n0 < window_end) {
+                        uint64_t words[BS_TREE_MAX_TOKENS / 64];
+                        const int begin = token_sees(a, seq, token_of(a, row0 + min((wr * NRB + rb) * 16 + col, n_rows - 1)), words);
+                        x = row_sees(n0, seq.base, begin, [&](int w) __attribute__((always_inline)) {
+                            const uint64_t y = w < 2 ? words[0] : w < 4 ? words[1] : w < 6 ? words[2] : words[3];
+                            return (uint32_t)(w & 1 ? y >> 32 : y);
+                        });
+                    }
                     seen[rb] = (x & exists) >> (4 * grp);
 #pragma unroll
                     for (int h = 0; h < SUB; ++h)
@@ -718,6 +726,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
 template <int D>
 struct Wide {
     static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves, kKeys = 32, kTurns = 1, kPerCu = 2;
+    static constexpr int kItem = 4;                           // (see Layout)
     static constexpr int kRowBytes = 2 * D, kBlock = kKeys * kRowBytes;                        // a block of K or V
     static constexpr int kLoads16 = 16 * kRowBytes / 1024;    // LDS-direct instructions per 16 slots, which lie in one page
     static constexpr int kSlots = D == 64 ? 8 : 4;            // blocks of K, of V, that the LDS holds
@@ -749,8 +758,8 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
 
     if (a.by_item)   // items that a sequence could have and has not: nothing to join
         for (int s = blockIdx.x; s < a.cache.n_seqs; s += gridDim.x)
-            for (int i = seq_of<KEYS, ROWS>(a, s, ScalarLoad{}).items + tid; i < a.most_items; i += THREADS) a.cuts[s * a.most_items + i] = Cut{s, i, 0, 0};
-    const Range range = own_range<KEYS, ROWS, 1, THREADS>(a, blockIdx.x, gridDim.x);
+            for (int i = seq_of<TR>(a, s, ScalarLoad{}).items + tid; i < a.most_items; i += THREADS) a.cuts[s * a.most_items + i] = Cut{s, i, 0, 0};
+    const Range range = own_range<TR>(a, blockIdx.x, gridDim.x);
     if (tid == 0 && !a.by_item) a.cuts[blockIdx.x] = Cut{0, -1, 0, 0};
     if (range.begin >= range.end) return;
 
@@ -794,14 +803,14 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
 
     Place at = range.at;
     int pos = range.begin;
-    Seq seq = seq_of<KEYS, ROWS>(a, at.seq, ScalarLoad{});
+    Seq seq = seq_of<TR>(a, at.seq, ScalarLoad{});
     while (pos < range.end) {
         while (at.item == seq.items) {   // the next sequence that has some
             at.item = 0;
-            seq = seq_of<KEYS, ROWS>(a, ++at.seq, ScalarLoad{});
+            seq = seq_of<TR>(a, ++at.seq, ScalarLoad{});
         }
-        const int block = max(0, at.unit - kItemBlocks);   // the first one
-        const int n_steps = min(seq.blocks - block, range.end - pos - max(0, kItemBlocks - at.unit));
+        const int block = max(0, at.unit - TR::kItem);   // the first one
+        const int n_steps = min(seq.blocks - block, range.end - pos - max(0, TR::kItem - at.unit));
         if (n_steps <= 0) break;   // the share ends where the item begins
         const int kvh = at.item / seq.groups, row0 = (at.item - kvh * seq.groups) * ROWS;   // rows: token by token, the group's heads of each
         const int n_rows = min(ROWS, seq.T * a.G - row0);
@@ -920,7 +929,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
                 s = x[0];
             }
             if (masked) {
-                seen = (row_sees<ROWS>(row_mask, row_begin, wave * 32 + n31, (b0 + i) * KEYS, seq.base) & exists) >> (4 * half);
+                seen = (row_sees((b0 + i) * KEYS, seq.base, row_begin[wave * 32 + n31], [&](int w) { return row_mask[w * ROWS + wave * 32 + n31]; }) & exists) >> (4 * half);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] = (seen & (1u << (8 * (e / 4) + e % 4))) ? s[e] : -INFINITY;
             }
@@ -1065,68 +1074,71 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
     }
 }
 
-// Joins the parts of a row (blockIdx.y) of an item that was cut (blockIdx.x): threads are D / 4 channel quads times the parts side by side, in a
+// Joins the parts of the rows of an item that was cut (blockIdx.x), every gridDim.y-th row: threads are D / 4 channel quads times the parts side by side, in a
 // fixed order.
-template <typename T, int D, int M>
+template <typename T, int D, typename L>
 __global__ __launch_bounds__(256) void tree_join(const TreeArgs a)
 {
-    constexpr int CH4 = D / 4, LANES = 256 / CH4;
+    constexpr int CH4 = D / 4, LANES = 256 / CH4, M = L::kRows;
     __shared__ float4 acc[LANES][CH4];
     __shared__ float2 ml[LANES];
-    const int tid = threadIdx.x, ch = tid % CH4, p0 = tid / CH4, row = blockIdx.y;
+    const int tid = threadIdx.x, ch = tid % CH4, p0 = tid / CH4;
     const Cut cut = a.cuts[blockIdx.x];
     if (a.by_item ? cut.first == cut.last : cut.item < 0) return;
-    const Seq seq = seq_of<sizeof(T) == 2 ? 32 : 16, M>(a, cut.seq, VectorLoad{});
-    const int kvh = cut.item / seq.groups, row0 = (cut.item - kvh * seq.groups) * M;
-    if (row >= min(M, seq.T * a.G - row0)) return;
+    const Seq seq = seq_of<L>(a, cut.seq, VectorLoad{});
+    const int kvh = cut.item / seq.groups, row0 = (cut.item - kvh * seq.groups) * M, n_rows = min(M, seq.T * a.G - row0);
     const float c = a.cap_log2e > 0.f ? a.cap_log2e : a.scale_log2e;
-    float m = -INFINITY, l = 0.f;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    // loads of eight parts go out together ; those behind the last one to that one
-    for (int w0 = cut.first + p0; w0 <= cut.last; w0 += 8 * LANES) {
-        float2 x[8];
-        float4 y[8];
+    for (int row = blockIdx.y; row < n_rows; row += gridDim.y) {
+        float m = -INFINITY, l = 0.f;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        // loads of eight parts go out together; those behind the last one to that one
+        for (int w0 = cut.first + p0; w0 <= cut.last; w0 += 8 * LANES) {
+            float2 x[8];
+            float4 y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int w = min(w0 + i * LANES, cut.last);
-            const int64_t at = (int64_t)(2 * w + (w == cut.first ? 1 : 0)) * M + row;
-            x[i] = a.part_ml[at];
-            y[i] = *reinterpret_cast<const float4 *>(a.part_o + at * D + 4 * ch);
+            for (int i = 0; i < 8; ++i) {
+                const int w = min(w0 + i * LANES, cut.last);
+                const int64_t at = (int64_t)(2 * w + (w == cut.first ? 1 : 0)) * M + row;
+                x[i] = a.part_ml[at];
+                y[i] = *reinterpret_cast<const float4 *>(a.part_o + at * D + 4 * ch);
+            }
+            const float m_old = m;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = fmaxf(m, x[i].x);
+            const float old = m_old == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_old - m) * c);
+            l *= old;
+            sum.x *= old; sum.y *= old; sum.z *= old; sum.w *= old;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (w0 + i * LANES > cut.last) continue;
+                const float f = x[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[i].x - m) * c);
+                l = fmaf(x[i].y, f, l);
+                sum.x = fmaf(y[i].x, f, sum.x); sum.y = fmaf(y[i].y, f, sum.y); sum.z = fmaf(y[i].z, f, sum.z); sum.w = fmaf(y[i].w, f, sum.w);
+            }
         }
-        const float m_old = m;
+        acc[p0][ch] = sum;
+        if (ch == 0) ml[p0] = make_float2(m, l);
+        __syncthreads();
+        if (tid < CH4) {
+            m = -INFINITY;
+            l = 0.f;
+            sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = fmaxf(m, x[i].x);
-        const float old = m_old == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_old - m) * c);
-        l *= old;
-        sum.x *= old; sum.y *= old; sum.z *= old; sum.w *= old;
+            for (int i = 0; i < LANES; ++i) m = fmaxf(m, ml[i].x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (w0 + i * LANES > cut.last) continue;
-            const float f = x[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[i].x - m) * c);
-            l = fmaf(x[i].y, f, l);
-            sum.x = fmaf(y[i].x, f, sum.x); sum.y = fmaf(y[i].y, f, sum.y); sum.z = fmaf(y[i].z, f, sum.z); sum.w = fmaf(y[i].w, f, sum.w);
+            for (int i = 0; i < LANES; ++i) {
+                const float g = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[i].x - m) * c);
+                const float4 y = acc[i][ch];
+                l = fmaf(ml[i].y, g, l);
+                sum.x = fmaf(y.x, g, sum.x); sum.y = fmaf(y.y, g, sum.y); sum.z = fmaf(y.z, g, sum.z); sum.w = fmaf(y.w, g, sum.w);
+            }
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const int R = row0 + row, t = token_of(a, R);
+            store_row4(static_cast<T *>(a.out) + (seq.token + t) * a.out_token + (int64_t)(kvh * a.G + R - t * a.G) * a.out_head + 4 * ch,
+                       make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
         }
+        __syncthreads();
     }
-    acc[p0][ch] = sum;
-    if (ch == 0) ml[p0] = make_float2(m, l);
-    __syncthreads();
-    if (tid >= CH4) return;
-    m = -INFINITY;
-    l = 0.f;
-    sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < LANES; ++i) m = fmaxf(m, ml[i].x);
-#pragma unroll
-    for (int i = 0; i < LANES; ++i) {
-        const float g = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[i].x - m) * c);
-        const float4 y = acc[i][ch];
-        l = fmaf(ml[i].y, g, l);
-        sum.x = fmaf(y.x, g, sum.x); sum.y = fmaf(y.y, g, sum.y); sum.z = fmaf(y.z, g, sum.z); sum.w = fmaf(y.w, g, sum.w);
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int R = row0 + row, t = token_of(a, R);
-    store_row4(static_cast<T *>(a.out) + (seq.token + t) * a.out_token + (int64_t)(kvh * a.G + R - t * a.G) * a.out_head + 4 * ch,
-               make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
 }
 
 // ------------------------------------------------------------------------------------ host
@@ -1166,19 +1178,18 @@ auto with_rows(int32_t M, F f)
     }
 }
 
-int32_t rows_of(int64_t rows, int32_t dtype)
+int32_t rows_of(int64_t rows)
 {
-    if (rows <= 32) return rows <= 16 ? 16 : 32;
-    return dtype == BS_F32 ? (rows <= 64 ? 64 : 128) : 128;
+    return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
 }
 
 // What the host has to know of the kernel's layout.
-struct Traits { int32_t keys, per_cu, turns; };
+struct Traits { int32_t rows, keys, per_cu, turns, item; };
 Traits traits_of(const bs_cache &c, int32_t M)
 {
     const auto get = [](auto k) {
         typedef typename decltype(k)::layout L;
-        return Traits{L::kKeys, L::kPerCu, L::kTurns};
+        return Traits{L::kRows, L::kKeys, L::kPerCu, L::kTurns, L::kItem};
     };
     if (c.dtype == BS_BF16) return c.head_dim == 64 ? with_rows<__bf16, 64>(M, get) : with_rows<__bf16, 128>(M, get);
     return c.head_dim == 64 ? with_rows<float, 64>(M, get) : with_rows<float, 128>(M, get);
@@ -1238,10 +1249,10 @@ int make_plan(const bs_cache &c, int32_t n_q_heads, int32_t n_tokens, int32_t ma
     const int32_t G = n_q_heads / c.n_kv_heads;
     const int64_t rows = (int64_t)G * std::min(std::max(1, n_tokens), max_tokens);   // of a sequence and KV head
     if (rows > 1 << 20) return BS_EUNSUPPORTED;   // (see token_of)
-    p->M = rows_of(rows, c.dtype);
-    const Traits t = traits_of(c, p->M);
+    const Traits t = traits_of(c, rows_of(rows));
+    p->M = t.rows;   // (the kernel's own, whatever was asked for)
     const int64_t groups = (rows + p->M - 1) / p->M, per_item = (cache_slots(c) + t.keys - 1) / t.keys + 1, items = (int64_t)c.n_seqs * c.n_kv_heads;
-    if (items > INT32_MAX / groups || items * groups > INT32_MAX / 2 / (per_item + kItemBlocks)) return BS_EUNSUPPORTED;   // units are counted in 32 bits
+    if (items > INT32_MAX / groups || items * groups > INT32_MAX / 2 / (per_item + t.item)) return BS_EUNSUPPORTED;   // units are counted in 32 bits
     p->most_items = (int32_t)(groups * c.n_kv_heads);
     p->n_shares = (int32_t)std::min<int64_t>((int64_t)n_cus * t.per_cu, (items * groups * per_item + t.turns - 1) / t.turns);
     const auto whole = [](int64_t bytes) { return (bytes + 255) / 256 * 256; };
@@ -1261,7 +1272,7 @@ int launch(const TreeArgs &a, const Plan &p, hipStream_t st)
         typedef typename K::layout L;
         hipError_t e = launch_kernel(K::kernel, dim3((unsigned)p.n_shares), dim3(L::kThreads), L::kLds, st, a);
         if (e != hipSuccess) return fail_hip(e, "tree_shares launch");
-        if (p.n_shares > 1) e = launch_kernel(tree_join<T, D, L::kRows>, dim3((unsigned)p.n_cuts, (unsigned)L::kRows), dim3(256), 0, st, a);
+        if (p.n_shares > 1) e = launch_kernel(tree_join<T, D, L>, dim3((unsigned)p.n_cuts, (unsigned)std::max(std::min(8, L::kRows), std::min(L::kRows, 4096 / p.n_cuts))), dim3(256), 0, st, a);
         return e == hipSuccess ? BS_OK : fail_hip(e, "tree_join launch");
     });
 }
