@@ -23,9 +23,9 @@
 namespace bs {
 namespace {
 
-// An item in more than one share: the first and the last workgroup that have a part of it.  Filed under the item where there are fewer items than shares
-// (first = last: a whole one), else under the first share (item -1: none goes on behind it).
-struct Cut { int32_t seq, item, first, last; };
+// An item in more than one share: the first and the last workgroup that have a part of it, and its rows: n_rows from row0 on of a KV head, of the sequence whose first
+// token is `token`.  Filed under the item where there are fewer items than shares, else under the first share; no rows: nothing to join.
+struct __align__(16) Cut { int32_t first, last, kvh, row0, n_rows, token, unused[2]; };
 
 struct TreeArgs {
     bs_cache cache;
@@ -273,10 +273,10 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
     // items that a sequence could have and has not: nothing to join
     if (a.by_item)
         for (int s = blockIdx.x; s < a.cache.n_seqs; s += gridDim.x)
-            for (int i = seq_of<TR>(a, s, ScalarLoad{}).items + tid; i < a.most_items; i += THREADS) a.cuts[s * a.most_items + i] = Cut{s, i, 0, 0};
+            for (int i = seq_of<TR>(a, s, ScalarLoad{}).items + tid; i < a.most_items; i += THREADS) a.cuts[s * a.most_items + i] = Cut{};
 
     const Range range = own_range<TR>(a, blockIdx.x, gridDim.x);
-    if (tid == 0 && !a.by_item) a.cuts[blockIdx.x] = Cut{0, -1, 0, 0};
+    if (tid == 0 && !a.by_item) a.cuts[blockIdx.x] = Cut{};
     if (range.begin >= range.end) return;
 
     typedef __attribute__((address_space(3))) void *lds_ptr;
@@ -714,7 +714,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
             }
         }
         if (begins && tid == 0 && (a.by_item || !ends))
-            a.cuts[a.by_item ? at.seq * a.most_items + at.item : (int)blockIdx.x] = Cut{at.seq, at.item, (int)blockIdx.x, (pos - at.unit + seq.units - 1) / range.each};
+            a.cuts[a.by_item ? at.seq * a.most_items + at.item : (int)blockIdx.x] = Cut{(int)blockIdx.x, (pos - at.unit + seq.units - 1) / range.each, kvh, row0, ends ? 0 : n_rows, seq.token, {}};
         pos += seq.units - at.unit;   // (behind the share's end if the item is cut)
         at.unit = 0;
         ++at.item;
@@ -758,9 +758,9 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
 
     if (a.by_item)   // items that a sequence could have and has not: nothing to join
         for (int s = blockIdx.x; s < a.cache.n_seqs; s += gridDim.x)
-            for (int i = seq_of<TR>(a, s, ScalarLoad{}).items + tid; i < a.most_items; i += THREADS) a.cuts[s * a.most_items + i] = Cut{s, i, 0, 0};
+            for (int i = seq_of<TR>(a, s, ScalarLoad{}).items + tid; i < a.most_items; i += THREADS) a.cuts[s * a.most_items + i] = Cut{};
     const Range range = own_range<TR>(a, blockIdx.x, gridDim.x);
-    if (tid == 0 && !a.by_item) a.cuts[blockIdx.x] = Cut{0, -1, 0, 0};
+    if (tid == 0 && !a.by_item) a.cuts[blockIdx.x] = Cut{};
     if (range.begin >= range.end) return;
 
     typedef __attribute__((address_space(3))) void *lds_ptr;
@@ -1066,7 +1066,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
             }
         }
         if (begins && tid == 0 && (a.by_item || !ends))
-            a.cuts[a.by_item ? at.seq * a.most_items + at.item : (int)blockIdx.x] = Cut{at.seq, at.item, (int)blockIdx.x, (pos - at.unit + seq.units - 1) / range.each};
+            a.cuts[a.by_item ? at.seq * a.most_items + at.item : (int)blockIdx.x] = Cut{(int)blockIdx.x, (pos - at.unit + seq.units - 1) / range.each, kvh, row0, ends ? 0 : n_rows, seq.token, {}};
         pos += seq.units - at.unit;   // (behind the share's end if the item is cut)
         at.unit = 0;
         ++at.item;
@@ -1074,8 +1074,8 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
     }
 }
 
-// Joins the parts of the rows of an item that was cut (blockIdx.x), every gridDim.y-th row: threads are D / 4 channel quads times the parts side by side, in a
-// fixed order.
+// Joins the parts of the rows of an item that was cut (blockIdx.x), in a fixed order.  Threads are D / 4 channel quads times the parts of a row side by side, or where
+// there are few parts times rows side by side, whichever takes fewer rounds of loads (a batch of 48, two to ten parts: 21 -> JOINUS us).
 template <typename T, int D, typename L>
 __global__ __launch_bounds__(256) void tree_join(const TreeArgs a)
 {
@@ -1084,58 +1084,65 @@ __global__ __launch_bounds__(256) void tree_join(const TreeArgs a)
     __shared__ float2 ml[LANES];
     const int tid = threadIdx.x, ch = tid % CH4, p0 = tid / CH4;
     const Cut cut = a.cuts[blockIdx.x];
-    if (a.by_item ? cut.first == cut.last : cut.item < 0) return;
-    const Seq seq = seq_of<L>(a, cut.seq, VectorLoad{});
-    const int kvh = cut.item / seq.groups, row0 = (cut.item - kvh * seq.groups) * M, n_rows = min(M, seq.T * a.G - row0);
     const float c = a.cap_log2e > 0.f ? a.cap_log2e : a.scale_log2e;
-    for (int row = blockIdx.y; row < n_rows; row += gridDim.y) {
-        float m = -INFINITY, l = 0.f;
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        // loads of eight parts go out together; those behind the last one to that one
-        for (int w0 = cut.first + p0; w0 <= cut.last; w0 += 8 * LANES) {
+    struct Sum { float m, l; float4 o; };
+    // every step-th part of a row: loads of eight go out together, those behind the last one to that one
+    const auto parts_of = [&](int row, int from, int step) {
+        Sum s{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+        for (int w0 = cut.first + from; w0 <= cut.last; w0 += 8 * step) {
             float2 x[8];
             float4 y[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int w = min(w0 + i * LANES, cut.last);
+                const int w = min(w0 + i * step, cut.last);
                 const int64_t at = (int64_t)(2 * w + (w == cut.first ? 1 : 0)) * M + row;
                 x[i] = a.part_ml[at];
                 y[i] = *reinterpret_cast<const float4 *>(a.part_o + at * D + 4 * ch);
             }
-            const float m_old = m;
+            const float m_old = s.m;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = fmaxf(m, x[i].x);
-            const float old = m_old == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_old - m) * c);
-            l *= old;
-            sum.x *= old; sum.y *= old; sum.z *= old; sum.w *= old;
+            for (int i = 0; i < 8; ++i) s.m = fmaxf(s.m, x[i].x);
+            const float old = m_old == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_old - s.m) * c);
+            s.l *= old;
+            s.o.x *= old; s.o.y *= old; s.o.z *= old; s.o.w *= old;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (w0 + i * LANES > cut.last) continue;
-                const float f = x[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[i].x - m) * c);
-                l = fmaf(x[i].y, f, l);
-                sum.x = fmaf(y[i].x, f, sum.x); sum.y = fmaf(y[i].y, f, sum.y); sum.z = fmaf(y[i].z, f, sum.z); sum.w = fmaf(y[i].w, f, sum.w);
+                if (w0 + i * step > cut.last) continue;
+                const float f = x[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[i].x - s.m) * c);
+                s.l = fmaf(x[i].y, f, s.l);
+                s.o.x = fmaf(y[i].x, f, s.o.x); s.o.y = fmaf(y[i].y, f, s.o.y); s.o.z = fmaf(y[i].z, f, s.o.z); s.o.w = fmaf(y[i].w, f, s.o.w);
             }
         }
-        acc[p0][ch] = sum;
-        if (ch == 0) ml[p0] = make_float2(m, l);
+        return s;
+    };
+    const auto finish = [&](int row, const Sum &s) {
+        const float inv = s.l == 0.f ? 0.f : 1.f / s.l;
+        const int R = cut.row0 + row, t = token_of(a, R);
+        store_row4(static_cast<T *>(a.out) + (cut.token + t) * a.out_token + (int64_t)(cut.kvh * a.G + R - t * a.G) * a.out_head + 4 * ch,
+                   make_float4(s.o.x * inv, s.o.y * inv, s.o.z * inv, s.o.w * inv));
+    };
+    const int n_parts = cut.last - cut.first + 1, y = gridDim.y, side = y * LANES;   // rounds of loads: rows side by side, or parts
+    if ((n_parts + 7) / 8 * ((cut.n_rows + side - 1) / side) <= (n_parts + 8 * LANES - 1) / (8 * LANES) * ((cut.n_rows + y - 1) / y)) {
+        for (int row = blockIdx.y * LANES + p0; row < cut.n_rows; row += gridDim.y * LANES) finish(row, parts_of(row, 0, 1));
+        return;
+    }
+    for (int row = blockIdx.y; row < cut.n_rows; row += gridDim.y) {
+        const Sum s = parts_of(row, p0, LANES);
+        acc[p0][ch] = s.o;
+        if (ch == 0) ml[p0] = make_float2(s.m, s.l);
         __syncthreads();
         if (tid < CH4) {
-            m = -INFINITY;
-            l = 0.f;
-            sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            Sum all{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll
-            for (int i = 0; i < LANES; ++i) m = fmaxf(m, ml[i].x);
+            for (int i = 0; i < LANES; ++i) all.m = fmaxf(all.m, ml[i].x);
 #pragma unroll
             for (int i = 0; i < LANES; ++i) {
-                const float g = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[i].x - m) * c);
+                const float g = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[i].x - all.m) * c);
                 const float4 y = acc[i][ch];
-                l = fmaf(ml[i].y, g, l);
-                sum.x = fmaf(y.x, g, sum.x); sum.y = fmaf(y.y, g, sum.y); sum.z = fmaf(y.z, g, sum.z); sum.w = fmaf(y.w, g, sum.w);
+                all.l = fmaf(ml[i].y, g, all.l);
+                all.o.x = fmaf(y.x, g, all.o.x); all.o.y = fmaf(y.y, g, all.o.y); all.o.z = fmaf(y.z, g, all.o.z); all.o.w = fmaf(y.w, g, all.o.w);
             }
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            const int R = row0 + row, t = token_of(a, R);
-            store_row4(static_cast<T *>(a.out) + (seq.token + t) * a.out_token + (int64_t)(kvh * a.G + R - t * a.G) * a.out_head + 4 * ch,
-                       make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+            finish(row, all);
         }
         __syncthreads();
     }
@@ -1272,7 +1279,7 @@ int launch(const TreeArgs &a, const Plan &p, hipStream_t st)
         typedef typename K::layout L;
         hipError_t e = launch_kernel(K::kernel, dim3((unsigned)p.n_shares), dim3(L::kThreads), L::kLds, st, a);
         if (e != hipSuccess) return fail_hip(e, "tree_shares launch");
-        if (p.n_shares > 1) e = launch_kernel(tree_join<T, D, L>, dim3((unsigned)p.n_cuts, (unsigned)std::max(std::min(8, L::kRows), std::min(L::kRows, 4096 / p.n_cuts))), dim3(256), 0, st, a);
+        if (p.n_shares > 1) e = launch_kernel(tree_join<T, D, L>, dim3((unsigned)p.n_cuts, (unsigned)std::max(8, std::min(L::kRows, 4096 / p.n_cuts))), dim3(256), 0, st, a);
         return e == hipSuccess ? BS_OK : fail_hip(e, "tree_join launch");
     });
 }
