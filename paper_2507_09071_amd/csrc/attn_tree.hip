@@ -1,14 +1,19 @@
 // Attention of a few drafted tokens per sequence (a tree or a chain) over a paged cache.
 //
 // K and V of a KV head are read once for the T tokens times G query heads that share them, so the work per byte grows with the tree: of a slot's 4 d bytes (bf16)
-// 4 d T G FLOP are made.  Up to about a hundred rows HBM bounds it, beyond that the matrix pipe; fp32 is bounded by the matrix pipe from a few dozen rows on.  How:
-//  * the T G rows of a sequence and KV head are cut into groups of at most M rows; an item is such a group.  M follows from max_tokens G: 16, 32 (four waves that each
-//    take every fourth block of 32 slots, on their own), 64, 128, 256 (eight waves: 2, 4, 8 of them share a block and have 32 rows each, in step).  More rows than
-//    M walk the cache again;
+// 4 d T G FLOP are made, 6 d T G with the probabilities in two numbers.  Up to some thirty rows (T G) HBM bounds it, beyond that what matrix and vector instructions
+// take; fp32 is bounded by the matrix pipe from sixteen rows on.  How:
+//  * the T G rows of a sequence and KV head are cut into groups of at most M rows; an item is such a group.  More rows than M walk the cache again.  Up to 32 rows
+//    four waves take every fourth block of slots each, on their own (tree_shares); more share their blocks and step together: in bf16 four waves of 32 rows
+//    (tree_wide), in fp32 two such groups of four.  Which when: rows_of, at the end;
 //  * the blocks of all items lie in one row that is cut into equal shares, one per workgroup, found on the device from the lengths; parts of items that were cut
 //    are joined by a second kernel in a fixed order;
 //  * masks cost nothing but at the end: slots below the length are seen by all, and only blocks that reach behind it (or hold the begin of a window, or a slot
-//    without a page) are masked, by 32 bits per row and block from a copy of the rows' masks in LDS.  A window is laid on the mask when it is copied.
+//    without a page) are masked, by 32 bits per row and block.  A window is laid on the words of a token's mask.
+// With 32 query heads on 8 of d 128 in bf16, beside 6.2 TB/s that a plain read reaches: two sequences of 150K slots, 128 rows each, 1.23 GB of K and V: 557 us with its
+// join, 610 before the matrix instructions had priority; its loads alone take 450, and what holds the rest back is power: the chip runs it at 1.5 to 1.67 of its
+// 2.4 GHz.  One of 39.5K slots and 182 rows, 162 MB in two walks: 41 us.  48 sequences of up to 20K slots and 30 rows with capped scores, 504 MB: 138 us, 113 without
+// the cap.
 #include "attn_common.h"
 #include "cache_attn.h"
 
@@ -50,14 +55,14 @@ template <typename T, int D, int NRB, int WR, int WK>
 struct Layout {
     static constexpr int kWaves = WR * WK, kThreads = 64 * kWaves, kRows = 16 * NRB * WR, kTurns = WK;
     static constexpr int kItem = 8;                           // beginning an item costs about as much as so many blocks: shares are equal with that counted
+                                                              // (and masks loaded late, 48 sequences of up to 30 rows: 168 -> 117 us)
     static constexpr int kKeys = sizeof(T) == 2 ? 32 : 16;    // slots of a block
     static constexpr int kRowBytes = D * (int)sizeof(T);
     static constexpr int kBlock = kKeys * kRowBytes;          // one block of K or V
     static constexpr int kLoads = kBlock / 1024;              // LDS-direct instructions per block
     static constexpr int kLoads16 = 16 * kRowBytes / 1024;    // ... per 16 slots, which lie in one page
     static constexpr int kOwn = (kLoads + WR - 1) / WR;       // ... of a wave
-    static constexpr int kStages = 2;
-    static constexpr int kGroup = kStages * 2 * kBlock;       // ring of a group of waves
+    static constexpr int kGroup = 2 * 2 * kBlock;             // ring of a group of waves: two blocks of K and V
     static constexpr int kQuery = WK * kGroup;                // the query rows behind the rings
     static constexpr int kMerge = WR > 1 ? kRows * D * 4 : kGroup;   // a group's results lie over the ring; where its waves have it alone, over its own part
     static constexpr int kEnd = kQuery + kRows * kRowBytes > WK * kMerge ? kQuery + kRows * kRowBytes : WK * kMerge;
@@ -264,7 +269,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
     using TR = Layout<T, D, NRB, WR, WK>;
     constexpr bool BF16 = sizeof(T) == 2, SHARED = WR > 1;
     constexpr int KEYS = TR::kKeys, ROWB = TR::kRowBytes, BLK = TR::kBlock, NI = TR::kLoads, NI16 = TR::kLoads16, SUB = KEYS / 16, OWN = TR::kOwn;
-    constexpr int ROWS = TR::kRows, NB = D / 16, CH4 = D / 4, WAVES = TR::kWaves, THREADS = TR::kThreads, STAGES = TR::kStages, KSTEPS = D * (int)sizeof(T) / 64;
+    constexpr int ROWS = TR::kRows, NB = D / 16, CH4 = D / 4, WAVES = TR::kWaves, THREADS = TR::kThreads, KSTEPS = D * (int)sizeof(T) / 64;
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, grp = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wk = wave / WR, wr = wave % WR;
@@ -396,7 +401,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
             issue(s0.k, ring);
             issue(s0.v, ring + BLK);
             s1 = sources_of(p1);
-            if (n_steps > 1 && (!SHARED || STAGES > 2)) {
+            if (!SHARED && n_steps > 1) {
                 issue(s1.k, ring + 2 * BLK);
                 issue(s1.v, ring + 3 * BLK);
             }
@@ -435,23 +440,13 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
             const int n0 = (b0 + WK * i) * KEYS;
             Sources s2{};
             if (SHARED) {
-                if (STAGES > 2 && more) wait_loads(std::integral_constant<int, 2 * OWN>{});
-                else wait_loads(std::integral_constant<int, 0>{});
+                wait_loads(std::integral_constant<int, 0>{});
                 meet();   // all of the block is there, and the stage of the block before is free
-                if constexpr (STAGES > 2) {
-                    if (more2) {
-                        s2 = sources_of(next);
-                        const int to = stage == 0 ? 4 * BLK : stage - 2 * BLK;
-                        issue(s2.k, ring + to);
-                        issue(s2.v, ring + to + BLK);
-                    }
-                } else {
-                    if (more) {
-                        issue(s1.k, ring + (stage ^ 2 * BLK));
-                        issue(s1.v, ring + (stage ^ 2 * BLK) + BLK);
-                    }
-                    if (more2) s1 = s2 = sources_of(next);
+                if (more) {
+                    issue(s1.k, ring + (stage ^ 2 * BLK));
+                    issue(s1.v, ring + (stage ^ 2 * BLK) + BLK);
                 }
+                if (more2) s1 = s2 = sources_of(next);
             } else if (more2) {
                 s2 = sources_of(next);
             }
@@ -610,7 +605,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
             const uint32_t fine = mine & ~bad;   // (a slot with a value that is not finite: all of its values)
             if constexpr (BF16) {
                 // Probabilities in two bf16 numbers each, 16 bits of their fraction.  One number would do half the work here, but is as coarse as the result's own
-                // rounding, which then is off by 1.4 times as much.
+                // rounding, which then is off by 1.4 times as much (two sequences of 150K slots: 580 -> 488 us).
                 bf16x8 pb[NRB], rest[NRB];
 #pragma unroll
                 for (int rb = 0; rb < NRB; ++rb)
@@ -656,7 +651,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
             }
             there0 = there1;
             there1 = s2.there;
-            stage = stage + 2 * BLK == STAGES * 2 * BLK ? 0 : stage + 2 * BLK;
+            stage ^= 2 * BLK;
         }
 
         // ---- the groups' results over the rings; [row][chunks of 4 channels, exchanged]
@@ -722,11 +717,12 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
     }
 }
 
-// Many rows (bf16): four waves of 32 rows each walk the same blocks of 32 slots in step; two such workgroups share a CU.
+// Many rows (bf16): four waves of 32 rows each walk the same blocks of 32 slots in step; two such workgroups share a CU, so that one has scores and probabilities
+// to make while the other waits for its waves.  Two waves load K and two load V, each three or more blocks ahead.
 template <int D>
 struct Wide {
     static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves, kKeys = 32, kTurns = 1, kPerCu = 2;
-    static constexpr int kItem = 4;                           // (see Layout)
+    static constexpr int kItem = 4;                           // (see Layout; 48 sequences of up to 30 rows here, with 2, 4, 8, 12: 168, 155, 160, 165 us)
     static constexpr int kRowBytes = 2 * D, kBlock = kKeys * kRowBytes;                        // a block of K or V
     static constexpr int kLoads16 = 16 * kRowBytes / 1024;    // LDS-direct instructions per 16 slots, which lie in one page
     static constexpr int kSlots = D == 64 ? 8 : 4;            // blocks of K, of V, that the LDS holds
@@ -850,8 +846,8 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
                 if (r < n) issue(number[r], at16[r]);
         };
 
-        // Two waves request the first keys, the others the query rows and what they see, in the layout of a K block and where values go later.  A place without a row holds a copy of the last
-        // one.
+        // Two waves request the first keys, the others the query rows, in the layout of a K block and where values go later, and find what they see.  A place without
+        // a row holds a copy of the last one.
         if (!values) {
             issue_first(min(RING, n_steps));
             if (n_steps < RING) wait_loads(std::integral_constant<int, 0>{});
@@ -990,12 +986,11 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
                     const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4)(lds + ((v_read[1] + from * BLK) ^ (cb << 6)) + j * 16 * ROWB)));
                     return __builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, y.x, y.y));
                 };
-                // the next block's scores (behind the last one: of whatever is there) beside this one's probabilities
-                bf16x8 vf[2][CB];
+                // The next block's scores (behind the last one: of whatever is there) beside this one's probabilities.  The first half of the values is read ahead of
+                // them, and the wave goes before those that are at their masks and references: both together 610 -> 557 us (two sequences of 150K slots).
+                bf16x8 vf[CB];
 #pragma unroll
-                for (int j = 0; j < 1; ++j)
-#pragma unroll
-                    for (int cb = 0; cb < CB; ++cb) vf[j][cb] = read_v(j, cb);
+                for (int cb = 0; cb < CB; ++cb) vf[cb] = read_v(0, cb);
                 __builtin_amdgcn_sched_barrier(0);
                 __builtin_amdgcn_s_setprio(1);
                 const floatx16 s_next = scores(next);
@@ -1019,7 +1014,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int cb = 0; cb < CB; ++cb) {
-                        const bf16x8 f = j == 0 ? vf[0][cb] : read_v(j, cb);
+                        const bf16x8 f = j == 0 ? vf[cb] : read_v(j, cb);
                         o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pb[j], o[cb], 0, 0, 0);
                         o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, rest[j], o[cb], 0, 0, 0);
                     }
@@ -1075,7 +1070,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
 }
 
 // Joins the parts of the rows of an item that was cut (blockIdx.x), in a fixed order.  Threads are D / 4 channel quads times the parts of a row side by side, or where
-// there are few parts times rows side by side, whichever takes fewer rounds of loads (a batch of 48, two to ten parts: 21 -> JOINUS us).
+// there are few parts times rows side by side, whichever takes fewer rounds of loads (a batch of 48, two to ten parts: 21 -> 8 us).
 template <typename T, int D, typename L>
 __global__ __launch_bounds__(256) void tree_join(const TreeArgs a)
 {
@@ -1175,19 +1170,25 @@ auto with_rows(int32_t M, F f)
         case 32: return f(Narrow<T, D, 2, 1, 4>{});
         default: return f(Broad<D>{});
         }
-    } else {   // (more rows, or more rings beside 64, do not fit the LDS)
+    } else {   // (more than 128 rows do not fit the LDS)
         switch (M) {
         case 16: return f(Narrow<T, D, 1, 1, 4>{});
         case 32: return f(Narrow<T, D, 2, 1, 4>{});
-        case 64: return f(Narrow<T, D, 2, 2, 2>{});
         default: return f(Narrow<T, D, 2, 4, 2>{});
         }
     }
 }
 
-int32_t rows_of(int64_t rows)
+// The M that a sequence's rows per KV head are cut by.  Measured with all of them, in us, 32 query heads on 8 of d 128; bf16: 16 sequences of 4K to 16K slots, fp32: 4
+// of 8K to 16K:
+//     rows           bf16: 16     32     40     64  |  fp32: 16     32     64    128
+//     M = 16            110.3  182.5  257.8  346.5  |      79.3  129.4  236.9  457.0
+//     M = 32            115.9  117.6  185.1  189.5  |      96.7   98.6  172.6  322.9
+//     M = 128           125.4  128.5  127.6  131.7  |     234.4  235.8  239.2  245.5
+// (64 rows in fp32 by four waves that share their blocks: 171.8.)
+int32_t rows_of(int32_t dtype, int64_t rows)
 {
-    return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+    return rows <= 16 ? 16 : rows <= (dtype == BS_BF16 ? 32 : 64) ? 32 : 128;
 }
 
 // What the host has to know of the kernel's layout.
@@ -1205,7 +1206,7 @@ Traits traits_of(const bs_cache &c, int32_t M)
 template <typename T, int D>
 hipError_t raise_limits()
 {
-    for (int M : {16, 32, 64, 128}) {
+    for (int M : {16, 32, 128}) {
         const hipError_t e = with_rows<T, D>(M, [](auto k) {
             typedef decltype(k) K;
             return hipFuncSetAttribute(reinterpret_cast<const void *>(K::kernel), hipFuncAttributeMaxDynamicSharedMemorySize, K::layout::kLds);
@@ -1256,8 +1257,8 @@ int make_plan(const bs_cache &c, int32_t n_q_heads, int32_t n_tokens, int32_t ma
     const int32_t G = n_q_heads / c.n_kv_heads;
     const int64_t rows = (int64_t)G * std::min(std::max(1, n_tokens), max_tokens);   // of a sequence and KV head
     if (rows > 1 << 20) return BS_EUNSUPPORTED;   // (see token_of)
-    const Traits t = traits_of(c, rows_of(rows));
-    p->M = t.rows;   // (the kernel's own, whatever was asked for)
+    const Traits t = traits_of(c, rows_of(c.dtype, rows));
+    p->M = t.rows;
     const int64_t groups = (rows + p->M - 1) / p->M, per_item = (cache_slots(c) + t.keys - 1) / t.keys + 1, items = (int64_t)c.n_seqs * c.n_kv_heads;
     if (items > INT32_MAX / groups || items * groups > INT32_MAX / 2 / (per_item + t.item)) return BS_EUNSUPPORTED;   // units are counted in 32 bits
     p->most_items = (int32_t)(groups * c.n_kv_heads);
