@@ -611,7 +611,7 @@ int64_t bs_attn_tree_workspace(const bs_cache *cache, int32_t n_q_heads, int32_t
 /*
  * Keep the drafted tokens that were accepted: slot lens[s] + i takes what slot lens[s] + path[s][i] held when the call began, K, V, weight and order, for
  * i < n_path[s], and lens_out[s] = lens[s] + n_path[s].  Other slots stay as they are, those of rejected tokens among them; they are free again.
- *   lens, lens_out   device [n_seqs], held within [0, max_pages * page_size]; may be the same
+ *   lens, lens_out   device [n_seqs], held within [0, max_pages * page_size]; may be the same, else lens_out overlaps nothing that is read
  *   path         device [n_seqs][max_path]: numbers of drafted tokens, in any order, one more than once too; where one is outside [0, BS_TREE_MAX_TOKENS), or either slot has
  *                no page, that slot stays as it is
  *   n_path       device [n_seqs], held within [0, max_path]

@@ -10,10 +10,10 @@
 //    are joined by a second kernel in a fixed order;
 //  * masks cost nothing but at the end: slots below the length are seen by all, and only blocks that reach behind it (or hold the begin of a window, or a slot
 //    without a page) are masked, by 32 bits per row and block.  A window is laid on the words of a token's mask.
-// With 32 query heads on 8 of d 128 in bf16, beside 6.2 TB/s that a plain read reaches: two sequences of 150K slots, 128 rows each, 1.23 GB of K and V: 557 us with its
-// join, 610 before the matrix instructions had priority; its loads alone take 450, and what holds the rest back is power: the chip runs it at 1.5 to 1.67 of its
-// 2.4 GHz.  One of 39.5K slots and 182 rows, 162 MB in two walks: 41 us.  48 sequences of up to 20K slots and 30 rows with capped scores, 504 MB: 138 us, 113 without
-// the cap.
+// With d 128 in bf16, where a plain read reaches 6.2 TB/s: two sequences of 150K slots, 16 KV heads, 128 rows of each, 2.47 GB of K and V: 557 us with its join, 610
+// before the matrix instructions had priority; its loads alone take 450, and what holds the rest back is power: the chip runs it at 1.5 to 1.67 of its 2.4 GHz.  One of
+// 39.5K slots, 4 KV heads, 182 rows, 81 MB that are walked twice: 41 us.  48 sequences of up to 16K slots, 8 KV heads, up to 80 rows, 504 MB, capped scores: 138 us, 113
+// without the cap.
 #include "attn_common.h"
 #include "cache_attn.h"
 
@@ -722,7 +722,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
 template <int D>
 struct Wide {
     static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves, kKeys = 32, kTurns = 1, kPerCu = 2;
-    static constexpr int kItem = 4;                           // (see Layout; 48 sequences of up to 30 rows here, with 2, 4, 8, 12: 168, 155, 160, 165 us)
+    static constexpr int kItem = 4;                           // (see Layout; 48 sequences of up to 80 rows with 2, 4, 8, 12: 168, 155, 160, 165 us)
     static constexpr int kRowBytes = 2 * D, kBlock = kKeys * kRowBytes;                        // a block of K or V
     static constexpr int kLoads16 = 16 * kRowBytes / 1024;    // LDS-direct instructions per 16 slots, which lie in one page
     static constexpr int kSlots = D == 64 ? 8 : 4;            // blocks of K, of V, that the LDS holds
@@ -1306,6 +1306,7 @@ extern "C" int bs_attn_tree(const bs_cache *cache, const bs_heads *q, const bs_h
     const bool none = n_tokens == 0;
     if (check_heads(q, none) || check_heads(out, none) || q->n_heads != out->n_heads || !first || !lens || window < 0) return BS_EINVAL;
     if (!(scale > 0.f) || !std::isfinite(scale) || !(cap >= 0.f) || !std::isfinite(cap)) return BS_EINVAL;
+    if (cap == 0.f && !std::isfinite(scale * 1.4426950408889634f)) return BS_EUNSUPPORTED;
     if (int rc = check_tree(cache, q->n_heads, n_tokens, max_tokens)) return rc;
     if (mask_words < 0 || (mask ? mask_words < (max_tokens + 63) / 64 : mask_words != 0) || (uintptr_t)mask % 8 != 0) return BS_EINVAL;
     if (!workspace || (uintptr_t)workspace % 16 != 0 || workspace_bytes < 0) return BS_EINVAL;

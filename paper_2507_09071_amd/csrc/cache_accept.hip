@@ -23,6 +23,9 @@ struct AcceptArgs {
     int64_t row_stride;
 };
 
+// Two arrays of int32 that share memory.
+bool overlap(const int32_t *x, int64_t n, const int32_t *y, int64_t m) { return x < y + m && y < x + n; }
+
 __device__ inline int held(int x, int lo, int hi) { return max(lo, min(x, hi)); }
 
 // blockIdx: x sequence, y KV head, z slices of K's rows, then of V's
@@ -95,6 +98,10 @@ extern "C" int bs_cache_accept(const bs_cache *cache, const int32_t *lens, int32
     if (int rc = check_cache(cache)) return rc;
     if (int rc = check_rows_apart(*cache)) return rc;
     if (!lens || !lens_out || !n_path || max_path < 0 || max_path > BS_TREE_MAX_TOKENS || (!path && max_path > 0)) return BS_EINVAL;
+    // the lengths that are written: in place of those that are read, or apart from all that is read
+    const int64_t n = cache->n_seqs;
+    if (lens_out != lens && overlap(lens_out, n, lens, n)) return BS_EINVAL;
+    if (overlap(lens_out, n, n_path, n) || overlap(lens_out, n, path, n * max_path)) return BS_EINVAL;
     if (slots)
         if (int rc = check_slots(*cache, slots)) return rc;
     if (cache->n_kv_heads > 65535) return BS_EUNSUPPORTED;   // of a grid

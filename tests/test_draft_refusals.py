@@ -52,7 +52,7 @@ def call_tree(**kw):
 
 
 def call_accept(**kw):
-    f = dict(cache=cache(), lens=P, lens_out=P, path=P, n_path=P, most=4, slots=None)
+    f = dict(cache=cache(), lens=P, lens_out=P, path=P + 4096, n_path=P + 8192, most=4, slots=None)
     f.update(kw)
     return binding.load_library().bs_cache_accept(ref(f["cache"]), f["lens"], f["lens_out"], f["path"], f["n_path"], f["most"], ref(f["slots"]), None)
 
@@ -117,7 +117,7 @@ def test_append(change):
     (dict(q=None), EINVAL), (dict(out=None), EINVAL), (dict(q=heads(data=None)), EINVAL), (dict(q=heads(6), out=heads(6)), EINVAL), (dict(out=heads(4)), EINVAL),
     (dict(q=heads(0), out=heads(0)), EINVAL), (dict(first=None), EINVAL), (dict(lens=None), EINVAL), (dict(n=-1), EINVAL), (dict(most=0), EINVAL), (dict(most=257), EINVAL),
     (dict(most=-1), EINVAL), (dict(words=1), EINVAL), (dict(words=-1), EINVAL), (dict(mask=None), EINVAL), (dict(mask=P + 4), EINVAL), (dict(window=-1), EINVAL),
-    (dict(scale=0.0), EINVAL), (dict(scale=math.nan), EINVAL), (dict(scale=math.inf), EINVAL), (dict(scale=-1.0), EINVAL), (dict(cap=-1.0), EINVAL), (dict(cap=math.nan), EINVAL),
+    (dict(scale=0.0), EINVAL), (dict(scale=math.nan), EINVAL), (dict(scale=math.inf), EINVAL), (dict(scale=-1.0), EINVAL), (dict(scale=3e38), EUNSUPPORTED), (dict(cap=-1.0), EINVAL), (dict(cap=math.nan), EINVAL),
     (dict(cap=math.inf), EINVAL), (dict(cap=3e38), EUNSUPPORTED), (dict(cap=1e-38, scale=1e30), EUNSUPPORTED), (dict(cap=1e30, scale=1e-30), EUNSUPPORTED),
     (dict(workspace=None), EINVAL), (dict(workspace=P + 8), EINVAL), (dict(n_bytes=-1), EINVAL), (dict(q=heads(data=P + 8)), EUNSUPPORTED), (dict(out=heads(head=132)), EUNSUPPORTED),
     (dict(out=heads(head=0)), EINVAL), (dict(out=heads(token=512)), EINVAL), (dict(q=heads(token=-8)), EINVAL), (dict(cache=cache(head_dim=256)), EUNSUPPORTED),
@@ -127,7 +127,8 @@ def test_tree(change, code):
 
 
 @pytest.mark.parametrize("change", [
-    dict(lens=None), dict(lens_out=None), dict(path=None), dict(n_path=None), dict(most=-1), dict(most=257), dict(slots=bs.CacheSlots(P, P, 111)), dict(slots=bs.CacheSlots(P + 2, P, 112))])
+    dict(lens=None), dict(lens_out=None), dict(path=None), dict(n_path=None), dict(most=-1), dict(most=257), dict(lens_out=P + 4), dict(lens=P + 4), dict(n_path=P), dict(path=P - 4),
+    dict(lens_out=P + 2048, path=P + 2048), dict(slots=bs.CacheSlots(P, P, 111)), dict(slots=bs.CacheSlots(P + 2, P, 112))])
 def test_accept(change):
     assert call_accept(**change) == EINVAL
 
