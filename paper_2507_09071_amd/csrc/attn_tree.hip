@@ -54,6 +54,7 @@ struct TreeArgs {
 template <typename T, int D, int NRB, int WR, int WK>
 struct Layout {
     static constexpr int kWaves = WR * WK, kThreads = 64 * kWaves, kRows = 16 * NRB * WR, kTurns = WK;
+    static constexpr int kEven = 0;
     static constexpr int kItem = 8;                           // beginning an item costs about as much as so many blocks: shares are equal with that counted
                                                               // (and masks loaded late, 48 sequences of up to 30 rows: 168 -> 117 us)
     static constexpr int kKeys = sizeof(T) == 2 ? 32 : 16;    // slots of a block
@@ -78,8 +79,8 @@ struct Layout {
 
 typedef float floatx8 __attribute__((ext_vector_type(8)));
 
-// A sequence: slots in use, its drafted tokens; what is visible of it, from block `first` on; units: of an item, with its beginning; items of it.
-struct Seq { int base, token, T, n, begin, first, blocks, units, groups, items; };
+// A sequence: slots in use, its drafted tokens; what is visible of it, from block `first` on; units: of an item, with its beginning; items of it, rows of an item.
+struct Seq { int base, token, T, n, begin, first, blocks, units, groups, items, rows; };
 
 template <typename L, typename LOAD>
 __device__ inline Seq seq_of(const TreeArgs &a, int s, LOAD load)
@@ -95,6 +96,10 @@ __device__ inline Seq seq_of(const TreeArgs &a, int s, LOAD load)
     v.blocks = (v.n + L::kKeys - 1) / L::kKeys - v.first;
     v.groups = (v.T * a.G + L::kRows - 1) / L::kRows;
     v.items = v.groups * a.cache.n_kv_heads;
+    // groups of like size, in whole waves: a share is as long for few rows as for many (8 sequences of 4K to 16K slots, 140 rows: 75 -> 70 us; 39.5K slots, 182 rows:
+    // 47.6 -> 46.5)
+    v.rows = L::kRows;
+    if (L::kEven > 0 && v.groups > 1) v.rows = ((v.T * a.G + v.groups - 1) / v.groups + L::kEven - 1) / L::kEven * L::kEven;
     v.units = v.T > 0 ? v.blocks + L::kItem : 0;
     return v;
 }
@@ -722,6 +727,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
 template <int D>
 struct Wide {
     static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves, kKeys = 32, kTurns = 1, kPerCu = 2;
+    static constexpr int kEven = 32;                          // rows of a wave
     static constexpr int kItem = 4;                           // (see Layout; 48 sequences of up to 80 rows with 2, 4, 8, 12: 168, 155, 160, 165 us)
     static constexpr int kRowBytes = 2 * D, kBlock = kKeys * kRowBytes;                        // a block of K or V
     static constexpr int kLoads16 = 16 * kRowBytes / 1024;    // LDS-direct instructions per 16 slots, which lie in one page
@@ -808,8 +814,8 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
         const int block = max(0, at.unit - TR::kItem);   // the first one
         const int n_steps = min(seq.blocks - block, range.end - pos - max(0, TR::kItem - at.unit));
         if (n_steps <= 0) break;   // the share ends where the item begins
-        const int kvh = at.item / seq.groups, row0 = (at.item - kvh * seq.groups) * ROWS;   // rows: token by token, the group's heads of each
-        const int n_rows = min(ROWS, seq.T * a.G - row0);
+        const int kvh = at.item / seq.groups, row0 = (at.item - kvh * seq.groups) * seq.rows;   // rows: token by token, the group's heads of each
+        const int n_rows = min(seq.rows, seq.T * a.G - row0);
         const int b0 = seq.first + block;
 
         // The wave's 16 slots of the next blocks that it requests (a page holds P16 such), and the place in the ring that they go to
