@@ -12,8 +12,8 @@
 //    without a page) are masked, by 32 bits per row and block.  A window is laid on the words of a token's mask.
 // With d 128 in bf16, where a plain read reaches 6.2 TB/s: two sequences of 150K slots, 16 KV heads, 128 rows of each, 2.47 GB of K and V: 557 us with its join, 610
 // before the matrix instructions had priority; its loads alone take 450, and what holds the rest back is power: the chip runs it at 1.5 to 1.67 of its 2.4 GHz.  One of
-// 39.5K slots, 4 KV heads, 182 rows, 81 MB that are walked twice: 41 us.  48 sequences of up to 16K slots, 8 KV heads, up to 80 rows, 504 MB, capped scores: 138 us, 113
-// without the cap.
+// 39.5K slots, 4 KV heads, 182 rows, 81 MB that are walked twice: 41 us.  48 sequences of up to 16K slots, 8 KV heads, up to 80 rows, 504 MB, capped scores: 126 us with
+// its join.
 #include "attn_common.h"
 #include "cache_attn.h"
 
@@ -78,6 +78,23 @@ struct Layout {
 
 
 typedef float floatx8 __attribute__((ext_vector_type(8)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// x as two bf16 numbers each, 16 bits of its fraction.  The first ones are taken apart again as the pairs that they are packed in (else each is rounded twice, once on
+// its own: two sequences of 150K slots 588 -> 576 us).
+__device__ inline void two_numbers(const floatx8 &x, bf16x8 &first, bf16x8 &rest)
+{
+    uint32_t a[4], b[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        a[w] = __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2){x[2 * w], x[2 * w + 1]}, bf16x2));
+        const floatx2 left = {x[2 * w] - __builtin_bit_cast(float, a[w] << 16), x[2 * w + 1] - __builtin_bit_cast(float, a[w] & 0xffff0000u)};
+        b[w] = __builtin_bit_cast(uint32_t, __builtin_convertvector(left, bf16x2));
+    }
+    first = __builtin_bit_cast(bf16x8, make_uint4(a[0], a[1], a[2], a[3]));
+    rest = __builtin_bit_cast(bf16x8, make_uint4(b[0], b[1], b[2], b[3]));
+}
 
 // A sequence: slots in use, its drafted tokens; what is visible of it, from block `first` on; units: of an item, with its beginning; items of it, rows of an item.
 struct Seq { int base, token, T, n, begin, first, blocks, units, groups, items, rows; };
@@ -181,9 +198,9 @@ __device__ inline Range own_range(const TreeArgs &a, int share, int n_shares)
     return r;
 }
 
-// tanh, in place, of scores times to_cap.  Below 1 a quotient of polynomials, the continued fraction of tanh after five terms (relative error 6e-8, at 1); capped scores are
-// that small as a rule, so it is tried alone, without the exponential.  From 1 on (e - 1) / (e + 1), e = exp(2 x): neither loses anything to a difference of
-// numbers that are alike.  (Beyond 15 tanh is 1 to the last bit; a NaN stays one.)
+// tanh, in place, of scores times to_cap.  Below 1/2 an odd polynomial with the least largest relative error there (1.5e-8); capped scores are that small as a rule, so it
+// is tried alone.  From 1/2 on 1 - 2 / (e + 1), e = exp(2 |x|), whose last difference makes the error of what is taken off 1.2 times as large at most; no e is too
+// large for it, and a NaN stays one.  No branch around a single score: with them the scores of a lane wait for each other (48 sequences of up to 80 rows: 143 -> 128 us).
 template <typename V, int N>
 __device__ inline void tanh_scores(V (&s)[N], float to_cap)
 {
@@ -196,19 +213,26 @@ __device__ inline void tanh_scores(V (&s)[N], float to_cap)
             s[n][e] *= to_cap;
             most = fmaxf(most, fabsf(s[n][e]));
         }
-    const bool small = __all(most < 1.f);
+    const auto near = [](float x) __attribute__((always_inline)) {
+        const float x2 = x * x;
+        return fmaf(x * x2, fmaf(x2, fmaf(x2, fmaf(x2, 0.01724148f, -0.05304549f), 0.13325879f), -0.33333144f), x);
+    };
+    if (__all(most < 0.5f)) {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < E; ++e) s[n][e] = near(s[n][e]);
+        return;
+    }
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float x = s[n][e], x2 = x * x;
-            float num = x * fmaf(x2, x2 + 105.f, 945.f), den = fmaf(x2, fmaf(x2, 15.f, 420.f), 945.f);
-            if (!small) {
-                const float y = x > 15.f ? 15.f : x < -15.f ? -15.f : x, z = __builtin_amdgcn_exp2f(y * 2.8853900817779268f);
-                num = x2 < 1.f ? num : z - 1.f;
-                den = x2 < 1.f ? den : z + 1.f;
-            }
-            s[n][e] = num * __builtin_amdgcn_rcpf(den);
+            const float x = s[n][e];
+            float small = near(x), large = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(fabsf(x) * 2.8853900817779268f) + 1.f), 1.f);
+            asm volatile("" : "+v"(small), "+v"(large));   // (both, by all lanes)
+            s[n][e] = fabsf(x) < 0.5f ? small : copysignf(large, x);
+            if (e % 2 == 1) __builtin_amdgcn_sched_barrier(0);   // (a few at a time: else they take too many registers; scores beyond half the cap 149 -> 145 us)
         }
 }
 
@@ -613,13 +637,12 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
                 // rounding, which then is off by 1.4 times as much (two sequences of 150K slots: 580 -> 488 us).
                 bf16x8 pb[NRB], rest[NRB];
 #pragma unroll
-                for (int rb = 0; rb < NRB; ++rb)
+                for (int rb = 0; rb < NRB; ++rb) {
+                    floatx8 x;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float x = p[rb][e >> 2][e & 3];
-                        pb[rb][e] = (__bf16)x;
-                        rest[rb][e] = (__bf16)(x - (float)pb[rb][e]);
-                    }
+                    for (int e = 0; e < 8; ++e) x[e] = p[rb][e >> 2][e & 3];
+                    two_numbers(x, pb[rb], rest[rb]);
+                }
                 uint32_t keep[4];
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
@@ -723,7 +746,8 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
 }
 
 // Many rows (bf16): four waves of 32 rows each walk the same blocks of 32 slots in step; two such workgroups share a CU, so that one has scores and probabilities
-// to make while the other waits for its waves.  Two waves load K and two load V, each three or more blocks ahead.
+// to make while the other waits for its waves.  Two waves load K and two load V, each three or more blocks ahead.  CAP: scores are capped (a kernel of its own: the
+// registers that a cap takes cost calls without one 3 %).
 template <int D>
 struct Wide {
     static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves, kKeys = 32, kTurns = 1, kPerCu = 2;
@@ -746,7 +770,7 @@ struct Wide {
     __device__ static int swizzle_v(int r) { return kRowBytes == 128 ? (r & 2) << 1 | ((r >> 2) & 3) : (r & 3) << 2 | ((r >> 2) & 3); }
 };
 
-template <int D>
+template <int D, bool CAP>
 __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
 {
     using TR = Wide<D>;
@@ -801,7 +825,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
     const uint32_t *row_mask = reinterpret_cast<const uint32_t *>(lds + TR::kMask);
     const int *row_begin = reinterpret_cast<const int *>(lds + TR::kBegin);
     uint32_t *flags = reinterpret_cast<uint32_t *>(lds + TR::kThere), *bad = reinterpret_cast<uint32_t *>(lds + TR::kBad);
-    const float c = a.cap_log2e > 0.f ? a.cap_log2e : a.scale_log2e;
+    const float c = CAP ? a.cap_log2e : a.scale_log2e;
 
     Place at = range.at;
     int pos = range.begin;
@@ -925,7 +949,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
         // ---- what the lane's row sees of it, and the row's reference point (see tree_shares); l and O follow it.  mx: of the scores as they come
         uint32_t seen = 0;
         const auto refer = [&](int i, float mx) __attribute__((always_inline)) {
-            if (a.cap_log2e > 0.f) {
+            if constexpr (CAP) {
                 floatx16 x[1] = {s};
                 tanh_scores(x, a.to_cap);
                 s = x[0];
@@ -935,7 +959,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] = (seen & (1u << (8 * (e / 4) + e % 4))) ? s[e] : -INFINITY;
             }
-            if (masked || a.cap_log2e > 0.f) mx = largest(s);
+            if (CAP || masked) mx = largest(s);
             mx = max_across_halves(mx);
             const bool grow = fmaf(mx, c, -(m_run * c)) > 8.f;
             if (__any(grow)) {
@@ -1011,8 +1035,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
                         x[e] = __builtin_amdgcn_exp2f(fmaf(s[8 * j + e], c, off));
                         sum[e & 1] += x[e];
                     }
-                    pb[j] = __builtin_convertvector(x, bf16x8);
-                    rest[j] = __builtin_convertvector(x - __builtin_convertvector(pb[j], floatx8), bf16x8);
+                    two_numbers(x, pb[j], rest[j]);
                 }
                 l_run += sum[0] + sum[1];
                 // ---- O^T += V^T P^T
@@ -1160,21 +1183,21 @@ struct Narrow {
     typedef Layout<T, D, NRB, WR, WK> layout;
     static constexpr auto kernel = tree_shares<T, D, NRB, WR, WK>;
 };
-template <int D>
+template <int D, bool CAP>
 struct Broad {
     typedef Wide<D> layout;
-    static constexpr auto kernel = tree_wide<D>;
+    static constexpr auto kernel = tree_wide<D, CAP>;
 };
 
-// The kernel for up to M rows of a sequence and KV head: f(its type).
+// The kernel for up to M rows of a sequence and KV head: f(its type).  `cap`: scores are capped.
 template <typename T, int D, typename F>
-auto with_rows(int32_t M, F f)
+auto with_rows(int32_t M, bool cap, F f)
 {
     if constexpr (sizeof(T) == 2) {
         switch (M) {
         case 16: return f(Narrow<T, D, 1, 1, 4>{});
         case 32: return f(Narrow<T, D, 2, 1, 4>{});
-        default: return f(Broad<D>{});
+        default: return cap ? f(Broad<D, true>{}) : f(Broad<D, false>{});
         }
     } else {   // (more than 128 rows do not fit the LDS)
         switch (M) {
@@ -1205,15 +1228,15 @@ Traits traits_of(const bs_cache &c, int32_t M)
         typedef typename decltype(k)::layout L;
         return Traits{L::kRows, L::kKeys, L::kPerCu, L::kTurns, L::kItem};
     };
-    if (c.dtype == BS_BF16) return c.head_dim == 64 ? with_rows<__bf16, 64>(M, get) : with_rows<__bf16, 128>(M, get);
-    return c.head_dim == 64 ? with_rows<float, 64>(M, get) : with_rows<float, 128>(M, get);
+    if (c.dtype == BS_BF16) return c.head_dim == 64 ? with_rows<__bf16, 64>(M, false, get) : with_rows<__bf16, 128>(M, false, get);
+    return c.head_dim == 64 ? with_rows<float, 64>(M, false, get) : with_rows<float, 128>(M, false, get);
 }
 
 template <typename T, int D>
 hipError_t raise_limits()
 {
-    for (int M : {16, 32, 128}) {
-        const hipError_t e = with_rows<T, D>(M, [](auto k) {
+    for (int i = 0; i < 4; ++i) {
+        const hipError_t e = with_rows<T, D>(i == 0 ? 16 : i == 1 ? 32 : 128, i == 3, [](auto k) {
             typedef decltype(k) K;
             return hipFuncSetAttribute(reinterpret_cast<const void *>(K::kernel), hipFuncAttributeMaxDynamicSharedMemorySize, K::layout::kLds);
         });
@@ -1281,7 +1304,7 @@ int make_plan(const bs_cache &c, int32_t n_q_heads, int32_t n_tokens, int32_t ma
 template <typename T, int D>
 int launch(const TreeArgs &a, const Plan &p, hipStream_t st)
 {
-    return with_rows<T, D>(p.M, [&](auto k) {
+    return with_rows<T, D>(p.M, a.cap_log2e > 0.f, [&](auto k) {
         typedef decltype(k) K;
         typedef typename K::layout L;
         hipError_t e = launch_kernel(K::kernel, dim3((unsigned)p.n_shares), dim3(L::kThreads), L::kLds, st, a);
