@@ -464,11 +464,11 @@ def _heads(x, n_tokens: int = 0, head_dim: int = 0, item: int = 0) -> bytes:
             return bytes(x)
         raise
     n_heads, tokens, channels = x.shape
-    if channel == 1 and tokens >= n_tokens and channels >= head_dim and (not item or x.element_size() == item):
-        return _pack_heads(x.data_ptr(), head, token, n_heads, 0)
     if channel != 1:
         raise ValueError("the channels of a head have to be contiguous")
-    raise ValueError(f"heads of shape {tuple(x.shape)} and {x.element_size()} bytes an element, where the call has {n_tokens} tokens, {head_dim} channels, {item} bytes")
+    if tokens < n_tokens or channels < head_dim or (item and x.element_size() != item):
+        raise ValueError(f"heads of shape {tuple(x.shape)} and {x.element_size()} bytes an element, where the call has {n_tokens} tokens, {head_dim} channels, {item} bytes")
+    return _pack_heads(x.data_ptr(), head, token, n_heads, 0)
 
 
 _ITEM = {BS_BF16: 2, BS_F32: 4}   # bytes; another dtype is the library's to refuse
@@ -477,18 +477,12 @@ _ITEM = {BS_BF16: 2, BS_F32: 4}   # bytes; another dtype is the library's to ref
 def _ints(x, n: int, name: str):
     """Address of at least n whole numbers of 32 bits, one behind the other (a tensor, an address, or None)."""
     try:
-        if x.element_size() == 4 and x.numel() >= n and x.is_contiguous():
-            return x.data_ptr()
+        fits = x.element_size() == 4 and x.numel() >= n and x.is_contiguous()
     except AttributeError:
         return None if x is None else int(x)
-    raise ValueError(f"{name} has to be contiguous int32, {n} numbers")
-
-
-def _rows(xs, n_tokens: int, head_dim: int, item: int) -> bytes:
-    """The bs_heads of one or two tensors, one behind the other."""
-    if len(xs) == 2:
-        return _heads(xs[0], n_tokens, head_dim, item) + _heads(xs[1], n_tokens, head_dim, item)
-    return b"".join([_heads(x, n_tokens, head_dim, item) for x in xs])
+    if not fits:
+        raise ValueError(f"{name} has to be contiguous int32, {n} numbers")
+    return x.data_ptr()
 
 
 def _positions(x, n_axes: int, n_tokens: int, axis_stride: int):
@@ -675,8 +669,7 @@ def _norm_ref(norm: Norm, head_dim: int, first: int, last: int):
     """Of the weights that a call with heads of head_dim channels looks at: numbers first .. last."""
     if last >= norm.n_weights:
         raise ValueError("a weight, or None, for each tensor")
-    sizes = norm.sizes
-    for n in (sizes[first], sizes[last]):
+    for n in norm.sizes[first:last + 1]:
         if n is not None and n != head_dim:
             raise ValueError(f"a weight of {n} channels, where the heads have {head_dim}")
     return ctypes.byref(norm)
@@ -689,8 +682,8 @@ def bs_norm_rope(norm: Norm, rope: Rope | None, xs, ys, dtype: int, n_tokens: in
     if len(ys) != n:
         raise ValueError("as many ys as xs")
     item, step = _ITEM.get(dtype, 0), n_tokens if axis_stride is None else int(axis_stride)
-    rc = load_library().bs_norm_rope(_norm_ref(norm, head_dim, 0, n - 1), _ref(rope), _rows(xs, n_tokens, head_dim, item), _rows(ys, n_tokens, head_dim, item), n,
-                                     int(dtype), n_tokens, head_dim,
+    rc = load_library().bs_norm_rope(_norm_ref(norm, head_dim, 0, n - 1), _ref(rope), b"".join([_heads(x, n_tokens, head_dim, item) for x in xs]),
+                                     b"".join([_heads(y, n_tokens, head_dim, item) for y in ys]), n, int(dtype), n_tokens, head_dim,
                                      None if rope is None else _positions(positions, rope.n_axes, n_tokens, step), step, int(stream) if stream else None)
     _check(rc, "bs_norm_rope")
 
@@ -703,7 +696,7 @@ def bs_norm_rope_grad(norm: Norm, rope: Rope | None, xs, dys, dxs, dweights, dty
     if len(dys) != n or len(dxs) != n:
         raise ValueError("as many dys and dxs as xs")
     item, step = _ITEM.get(dtype, 0), n_tokens if axis_stride is None else int(axis_stride)
-    rows = [_rows(group, n_tokens, head_dim, item) for group in (xs, dys, dxs)]
+    rows = [b"".join([_heads(x, n_tokens, head_dim, item) for x in group]) for group in (xs, dys, dxs)]
     rc = load_library().bs_norm_rope_grad(_norm_ref(norm, head_dim, 0, n - 1), _ref(rope), *rows, _floats(dweights, n * head_dim, "dweights"), n, int(dtype), n_tokens,
                                           head_dim, None if rope is None else _positions(positions, rope.n_axes, n_tokens, step), step,
                                           *((None, 0) if workspace is None else _buffer(workspace)), int(stream) if stream else None)
