@@ -55,8 +55,9 @@ template <typename T, int D, int NRB, int WR, int WK>
 struct Layout {
     static constexpr int kWaves = WR * WK, kThreads = 64 * kWaves, kRows = 16 * NRB * WR, kTurns = WK;
     static constexpr int kEven = 0;
-    static constexpr int kItem = 8;                           // beginning an item costs about as much as so many blocks: shares are equal with that counted
-                                                              // (and masks loaded late, 48 sequences of up to 30 rows: 168 -> 117 us)
+    static constexpr int kItem = 10;                          // beginning an item costs about as much as so many blocks: shares are equal with that counted
+                                                              // (200 sequences of 200 to 2K slots, 16 rows, with 4, 6, 8, 10, 12, 16: 147, 138, 135, 130, 131,
+                                                              // 134 us; 48 of up to 16K, 30 rows: 149, 124, 112, 112, 113, 114)
     static constexpr int kKeys = sizeof(T) == 2 ? 32 : 16;    // slots of a block
     static constexpr int kRowBytes = D * (int)sizeof(T);
     static constexpr int kBlock = kKeys * kRowBytes;          // one block of K or V
@@ -752,7 +753,7 @@ template <int D>
 struct Wide {
     static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves, kKeys = 32, kTurns = 1, kPerCu = 2;
     static constexpr int kEven = 32;                          // rows of a wave
-    static constexpr int kItem = 4;                           // (see Layout; 48 sequences of up to 80 rows with 2, 4, 8, 12: 168, 155, 160, 165 us)
+    static constexpr int kItem = 4;                           // (see Layout; 48 sequences of up to 80 rows with 2, 3, 4, 5, 6, 8: 149, 131, 124, 126, 126, 127 us)
     static constexpr int kRowBytes = 2 * D, kBlock = kKeys * kRowBytes;                        // a block of K or V
     static constexpr int kLoads16 = 16 * kRowBytes / 1024;    // LDS-direct instructions per 16 slots, which lie in one page
     static constexpr int kSlots = D == 64 ? 8 : 4;            // blocks of K, of V, that the LDS holds
