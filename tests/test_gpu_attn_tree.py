@@ -156,6 +156,28 @@ def test_capped_scores(dtype, hq, cap, scale):
     run(Drafts(dtype, 2, 128, 16, [400, 33, 90], counts, trees(counts), seed=10), hq, cap=cap, scale=scale)
 
 
+@pytest.mark.parametrize("dtype,hq", [("bf16", 8), ("f32", 8), ("bf16", 70)])
+def test_small_scores_beside_capped_ones(dtype, hq):
+    """Every other token has scores of a thousand times the others', far beyond the cap: the others keep the tolerance of their own scores."""
+    counts = [6, 1, 12]
+    d = Drafts(dtype, 2, 128, 16, [200, 31, 500], counts, trees(counts), seed=14)
+    q, scale, cap = draw_q(d, hq), 128 ** -0.5, 300.0
+    large = torch.arange(d.n) % 2 == 1
+    q[large] *= 1000
+    dev = q.to(DEV)
+    out = torch.empty_like(dev)
+    mask = torch.cat([words_of(b, 1) for b in d.bits]).to(DEV)
+    first = torch.from_numpy(d.first.astype(np.int32)).to(DEV)
+    ws = torch.empty(bs.bs_attn_tree_workspace(d.c.cache, hq, d.n, d.most), dtype=torch.uint8, device=DEV)
+    bs.bs_attn_tree(d.c.cache, dev.transpose(0, 1), out.transpose(0, 1), d.n, first, d.lens, d.most, scale, ws, mask=mask, cap=cap, stream=stream())
+    want, spread, _ = d.expect(q.double().numpy(), scale, 0, cap)
+    small = ~large.numpy()
+    S = d.expect(torch.where(large[:, None, None], torch.zeros_like(q), q).double().numpy(), scale, 0, cap)[2]
+    got = out.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    assert (np.abs(got - want)[small] <= bounds(dtype, 128, S, 512, want, spread)[small]).all()
+
+
 def test_large_scores():
     run(Drafts("bf16", 2, 128, 16, [1000, 50], [5, 9], None, seed=11), 8, scale=3.0)
     run(Drafts("f32", 2, 64, 16, [1000, 50], [5, 9], None, seed=11), 8, scale=3.0)
