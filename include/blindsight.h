@@ -599,8 +599,8 @@ int64_t bs_attn_decode_workspace(const bs_cache *cache, int32_t n_q_heads, int32
  *   cap          >= 0; 0: none
  *   workspace    at least bs_attn_tree_workspace bytes, 16-byte aligned
  * Slots that no token sees may hold anything, infinities and NaN too, and a slot that only some see leaves the others as they are; one with such a value
- * can make the rows that see it not finite.  Scores, sums and probabilities are fp32; bf16: each probability goes into P V as two bf16 numbers, off by at most
- * 2^-16 of itself; the result is rounded once.  Same inputs, same bits.
+ * can make the rows that see it not finite.  Probabilities (bf16: as three bf16 numbers each), scores and sums are fp32; the result is rounded once.  Same inputs,
+ * same bits.
  */
 int bs_attn_tree(const bs_cache *cache, const bs_heads *q, const bs_heads *out, int32_t n_tokens, const int32_t *first, const int32_t *lens, int32_t max_tokens,
                  const uint64_t *mask, int32_t mask_words, int32_t window, float scale, float cap, void *workspace, int64_t workspace_bytes, void *stream);

@@ -1,7 +1,7 @@
 // Attention of a few drafted tokens per sequence (a tree or a chain) over a paged cache.
 //
 // K and V of a KV head are read once for the T tokens times G query heads that share them, so the work per byte grows with the tree: of a slot's 4 d bytes (bf16)
-// 4 d T G FLOP are made, 6 d T G with the probabilities in two numbers.  Up to some thirty rows (T G) HBM bounds it, beyond that what matrix and vector instructions
+// 4 d T G FLOP are made, 8 d T G with the probabilities in three numbers.  Up to some thirty rows (T G) HBM bounds it, beyond that what matrix and vector instructions
 // take; fp32 is bounded by the matrix pipe from sixteen rows on.  How:
 //  * the T G rows of a sequence and KV head are cut into groups of at most M rows; an item is such a group.  More rows than M walk the cache again.  Up to 32 rows
 //    four waves take every fourth block of slots each, on their own (tree_shares); more share their blocks and step together: in bf16 four waves of 32 rows
@@ -10,10 +10,9 @@
 //    are joined by a second kernel in a fixed order;
 //  * masks cost nothing but at the end: slots below the length are seen by all, and only blocks that reach behind it (or hold the begin of a window, or a slot
 //    without a page) are masked, by 32 bits per row and block.  A window is laid on the words of a token's mask.
-// With d 128 in bf16, where a plain read reaches 6.2 TB/s: two sequences of 150K slots, 16 KV heads, 128 rows of each, 2.47 GB of K and V: 557 us with its join, 610
-// before the matrix instructions had priority; its loads alone take 450, and what holds the rest back is power: the chip runs it at 1.5 to 1.67 of its 2.4 GHz.  One of
-// 39.5K slots, 4 KV heads, 182 rows, 81 MB that are walked twice: 41 us.  48 sequences of up to 16K slots, 8 KV heads, up to 80 rows, 504 MB, capped scores: 126 us with
-// its join.
+// With d 128 in bf16, where a plain read reaches 6.2 TB/s, joins included: two sequences of 150K slots, 16 KV heads, 128 rows of each, 2.47 GB of K and V: 665 us; its
+// loads alone take 450, and what holds the rest back is power, of which the products of the probabilities' three numbers take their share (two numbers: 578).  One of
+// 39.5K slots, 4 KV heads, 182 rows, 81 MB that are walked twice: 49 us.  48 sequences of up to 16K slots, 8 KV heads, up to 80 rows, 504 MB, capped scores: 126 us.
 #include "attn_common.h"
 #include "cache_attn.h"
 
@@ -56,8 +55,8 @@ struct Layout {
     static constexpr int kWaves = WR * WK, kThreads = 64 * kWaves, kRows = 16 * NRB * WR, kTurns = WK;
     static constexpr int kEven = 0;
     static constexpr int kItem = 10;                          // beginning an item costs about as much as so many blocks: shares are equal with that counted
-                                                              // (200 sequences of 200 to 2K slots, 16 rows, with 4, 6, 8, 10, 12, 16: 147, 138, 135, 130, 131,
-                                                              // 134 us; 48 of up to 16K, 30 rows: 149, 124, 112, 112, 113, 114)
+                                                              // (200 sequences of 200 to 2K slots, 16 rows, with 4, 6, 8, 10, 12, 16: 152, 144, 139, 136, 138,
+                                                              // 140 us; 48 of up to 16K, 30 rows: 169, 140, 123, 115, 114, 117)
     static constexpr int kKeys = sizeof(T) == 2 ? 32 : 16;    // slots of a block
     static constexpr int kRowBytes = D * (int)sizeof(T);
     static constexpr int kBlock = kKeys * kRowBytes;          // one block of K or V
@@ -82,19 +81,27 @@ typedef float floatx8 __attribute__((ext_vector_type(8)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// x as two bf16 numbers each, 16 bits of its fraction.  The first ones are taken apart again as the pairs that they are packed in (else each is rounded twice, once on
-// its own: two sequences of 150K slots 588 -> 576 us).
-__device__ inline void two_numbers(const floatx8 &x, bf16x8 &first, bf16x8 &rest)
+// x as three bf16 numbers each, which hold all 24 bits of its fraction: what each leaves over is exact.  Where values cancel, nothing is left of a row but what its
+// probabilities have lost: with two numbers 2.7e-6 of sum p |v|, five times what products of fp32 may be off.  Both sides, two and three: up to 32 rows the same time (16
+// sequences of 4K to 16K slots 117 / 115 us, 32 rows 124 / 120), 64 rows 132 / 135, 128 rows 159 / 176, two sequences of 150K slots 578 / 664.
+// The numbers are taken apart again as the pairs that they are packed in (else each is rounded twice, once on its own).
+__device__ inline void three_numbers(const floatx8 &x, bf16x8 &first, bf16x8 &rest, bf16x8 &last)
 {
-    uint32_t a[4], b[4];
+    uint32_t a[4], b[4], c[4];
+    const auto less = [](floatx2 y, uint32_t pair) __attribute__((always_inline)) {
+        return (floatx2){y[0] - __builtin_bit_cast(float, pair << 16), y[1] - __builtin_bit_cast(float, pair & 0xffff0000u)};
+    };
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        a[w] = __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2){x[2 * w], x[2 * w + 1]}, bf16x2));
-        const floatx2 left = {x[2 * w] - __builtin_bit_cast(float, a[w] << 16), x[2 * w + 1] - __builtin_bit_cast(float, a[w] & 0xffff0000u)};
+        const floatx2 y = {x[2 * w], x[2 * w + 1]};
+        a[w] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
+        const floatx2 left = less(y, a[w]);
         b[w] = __builtin_bit_cast(uint32_t, __builtin_convertvector(left, bf16x2));
+        c[w] = __builtin_bit_cast(uint32_t, __builtin_convertvector(less(left, b[w]), bf16x2));
     }
     first = __builtin_bit_cast(bf16x8, make_uint4(a[0], a[1], a[2], a[3]));
     rest = __builtin_bit_cast(bf16x8, make_uint4(b[0], b[1], b[2], b[3]));
+    last = __builtin_bit_cast(bf16x8, make_uint4(c[0], c[1], c[2], c[3]));
 }
 
 // A sequence: slots in use, its drafted tokens; what is visible of it, from block `first` on; units: of an item, with its beginning; items of it, rows of an item.
@@ -233,7 +240,7 @@ __device__ inline void tanh_scores(V (&s)[N], float to_cap)
             float small = near(x), large = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(fabsf(x) * 2.8853900817779268f) + 1.f), 1.f);
             asm volatile("" : "+v"(small), "+v"(large));   // (both, by all lanes)
             s[n][e] = fabsf(x) < 0.5f ? small : copysignf(large, x);
-            if (e % 2 == 1) __builtin_amdgcn_sched_barrier(0);   // (a few at a time: else they take too many registers; scores beyond half the cap 149 -> 145 us)
+            if (e % 2 == 1) __builtin_amdgcn_sched_barrier(0);   // (a few at a time: else they take too many registers; scores beyond half the cap 153 -> 149 us)
         }
 }
 
@@ -634,15 +641,14 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
             }
             const uint32_t fine = mine & ~bad;   // (a slot with a value that is not finite: all of its values)
             if constexpr (BF16) {
-                // Probabilities in two bf16 numbers each, 16 bits of their fraction.  One number would do half the work here, but is as coarse as the result's own
-                // rounding, which then is off by 1.4 times as much (two sequences of 150K slots: 580 -> 488 us).
-                bf16x8 pb[NRB], rest[NRB];
+                // Probabilities in three bf16 numbers each: where values cancel, nothing is left but what a probability has lost.
+                bf16x8 pb[NRB], rest[NRB], last[NRB];
 #pragma unroll
                 for (int rb = 0; rb < NRB; ++rb) {
                     floatx8 x;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] = p[rb][e >> 2][e & 3];
-                    two_numbers(x, pb[rb], rest[rb]);
+                    three_numbers(x, pb[rb], rest[rb], last[rb]);
                 }
                 uint32_t keep[4];
 #pragma unroll
@@ -658,6 +664,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
                     for (int rb = 0; rb < NRB; ++rb) {
                         o[rb][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), pb[rb], o[rb][nb], 0, 0, 0);
                         o[rb][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), rest[rb], o[rb][nb], 0, 0, 0);
+                        o[rb][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), last[rb], o[rb][nb], 0, 0, 0);
                     }
                 }
             } else {
@@ -753,7 +760,7 @@ template <int D>
 struct Wide {
     static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves, kKeys = 32, kTurns = 1, kPerCu = 2;
     static constexpr int kEven = 32;                          // rows of a wave
-    static constexpr int kItem = 4;                           // (see Layout; 48 sequences of up to 80 rows with 2, 3, 4, 5, 6, 8: 149, 131, 124, 126, 126, 127 us)
+    static constexpr int kItem = 4;                           // (see Layout; 48 sequences of up to 80 rows with 2, 3, 4, 5, 6, 8: 151, 133, 127, 128, 128, 129 us)
     static constexpr int kRowBytes = 2 * D, kBlock = kKeys * kRowBytes;                        // a block of K or V
     static constexpr int kLoads16 = 16 * kRowBytes / 1024;    // LDS-direct instructions per 16 slots, which lie in one page
     static constexpr int kSlots = D == 64 ? 8 : 4;            // blocks of K, of V, that the LDS holds
@@ -1018,7 +1025,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
                     return __builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, y.x, y.y));
                 };
                 // The next block's scores (behind the last one: of whatever is there) beside this one's probabilities.  The first half of the values is read ahead of
-                // them, and the wave goes before those that are at their masks and references: both together 610 -> 557 us (two sequences of 150K slots).
+                // them, and the wave goes before those that are at their masks and references: both together 682 -> 647 us (two sequences of 150K slots).
                 bf16x8 vf[CB];
 #pragma unroll
                 for (int cb = 0; cb < CB; ++cb) vf[cb] = read_v(0, cb);
@@ -1027,7 +1034,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
                 const floatx16 s_next = scores(next);
                 const float off = m_run == -INFINITY ? 0.f : -(m_run * c);   // no slot so far: p = 0
                 float sum[2] = {0.f, 0.f};
-                bf16x8 pb[2], rest[2];   // of 16 slots each, as two numbers (see tree_shares)
+                bf16x8 pb[2], rest[2], last[2];   // of 16 slots each, as three numbers (see tree_shares)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     floatx8 x;
@@ -1036,7 +1043,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
                         x[e] = __builtin_amdgcn_exp2f(fmaf(s[8 * j + e], c, off));
                         sum[e & 1] += x[e];
                     }
-                    two_numbers(x, pb[j], rest[j]);
+                    three_numbers(x, pb[j], rest[j], last[j]);
                 }
                 l_run += sum[0] + sum[1];
                 // ---- O^T += V^T P^T
@@ -1047,6 +1054,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide(const TreeArgs a)
                         const bf16x8 f = j == 0 ? vf[cb] : read_v(j, cb);
                         o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pb[j], o[cb], 0, 0, 0);
                         o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, rest[j], o[cb], 0, 0, 0);
+                        o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, last[j], o[cb], 0, 0, 0);
                     }
                 __builtin_amdgcn_s_setprio(0);
                 s = s_next;
@@ -1209,13 +1217,16 @@ auto with_rows(int32_t M, bool cap, F f)
     }
 }
 
-// The M that a sequence's rows per KV head are cut by.  Measured with all of them, in us, 32 query heads on 8 of d 128; bf16: 16 sequences of 4K to 16K slots, fp32: 4
+// The M that a sequence's rows per KV head are cut by.  Measured with all of them, in us, 32 query heads on 8; bf16: 16 sequences of 4K to 16K slots, fp32: 4
 // of 8K to 16K:
-//     rows           bf16: 16     32     40     64  |  fp32: 16     32     64    128
-//     M = 16            110.3  182.5  257.8  346.5  |      79.3  129.4  236.9  457.0
-//     M = 32            115.9  117.6  185.1  189.5  |      96.7   98.6  172.6  322.9
-//     M = 128           125.4  128.5  127.6  131.7  |     234.4  235.8  239.2  245.5
-// (64 rows in fp32 by four waves that share their blocks: 171.8.)
+//              rows    bf16: 16     32     40     64    128  |  fp32: 16     32     64    128
+//     d 128, M = 16       113.6  187.9  268.9  353.3  683.9  |      80.7  132.5  244.5  482.0
+//            M = 32       119.2  120.0  189.6  193.7  370.1  |      96.2   99.6  175.7  332.4
+//            M = 128      122.8  126.0  128.3  134.0  171.2  |     244.6  248.1  250.3  256.1
+//     d 64,  M = 16        63.4   99.5  140.8  183.4  355.9  |      47.3   72.1  131.0  252.1
+//            M = 32        66.7   68.9  103.4  105.9  192.3  |      51.0   51.8   84.7  147.7
+//            M = 128       79.9   81.9   94.9   96.3  113.1  |     140.6  141.3  143.9  148.1
+// (64 rows of d 128 in fp32 by four waves that share their blocks: no less than twice 32.)
 int32_t rows_of(int32_t dtype, int64_t rows)
 {
     return rows <= 16 ? 16 : rows <= (dtype == BS_BF16 ? 32 : 64) ? 32 : 128;
