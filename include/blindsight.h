@@ -598,6 +598,7 @@ int64_t bs_attn_decode_workspace(const bs_cache *cache, int32_t n_q_heads, int32
  *   window       > 0: of the slots that a token sees by the above, only the last `window`
  *   cap          >= 0; 0: none
  *   workspace    at least bs_attn_tree_workspace bytes, 16-byte aligned
+ * n_tokens may be 0, and pointers to q, out and the mask null then (as of bs_cache_append).
  * Slots that no token sees may hold anything, infinities and NaN too, and a slot that only some see leaves the others as they are; one with such a value
  * can make the rows that see it not finite.  Probabilities (bf16: as three bf16 numbers each), scores and sums are fp32; the result is rounded once.  Same inputs,
  * same bits.

@@ -1349,7 +1349,7 @@ extern "C" int bs_attn_tree(const bs_cache *cache, const bs_heads *q, const bs_h
     if (!(scale > 0.f) || !std::isfinite(scale) || !(cap >= 0.f) || !std::isfinite(cap)) return BS_EINVAL;
     if (cap == 0.f && !std::isfinite(scale * 1.4426950408889634f)) return BS_EUNSUPPORTED;
     if (int rc = check_tree(cache, q->n_heads, n_tokens, max_tokens)) return rc;
-    if (mask_words < 0 || (mask ? mask_words < (max_tokens + 63) / 64 : mask_words != 0) || (uintptr_t)mask % 8 != 0) return BS_EINVAL;
+    if (mask_words < 0 || (mask ? mask_words < (max_tokens + 63) / 64 : mask_words != 0 && !none) || (uintptr_t)mask % 8 != 0) return BS_EINVAL;   // (an empty mask's address is null)
     if (!workspace || (uintptr_t)workspace % 16 != 0 || workspace_bytes < 0) return BS_EINVAL;
     if (!rows_aligned(*q, cache->dtype) || !rows_aligned(*out, cache->dtype)) return BS_EUNSUPPORTED;
     if (int rc = check_rows_apart(*out, n_tokens, cache->head_dim)) return rc;
