@@ -476,6 +476,7 @@ int bs_rope_init(bs_rope *rope, int32_t rotary_dim, int32_t layout, double base,
  * at 2^31.  The product is fp32, rounded
  * once.  Any alignment and stride; 16-byte loads are used where pointers, strides and sizes allow them.  n_tokens may be 0, and pointers to
  * data, positions and lists of tokens null then (as of bs_cache_append).
+ * BS_EUNSUPPORTED for more than 2^31 - 1 pieces, n_tokens times those of a row: head_dim / 2 channels in loads of up to 16 bytes.
  */
 int bs_rope_apply(const bs_rope *rope, const bs_heads *x, const bs_heads *y, int32_t n_tensors, int32_t dtype, int32_t n_tokens,
                   int32_t head_dim, const int32_t *positions, int64_t axis_stride, uint32_t flags, void *stream);
@@ -527,7 +528,8 @@ typedef struct {
 
 /*
  * Norm of every head and the rotary positions behind it in one pass: bs_rope_apply of the normed rows, which are not rounded in between.
- * Arguments as those of bs_rope_apply; rope NULL: no rotation (positions are not looked at then).  y may be x.
+ * Arguments as those of bs_rope_apply; rope NULL: no rotation (positions are not looked at then).  y may be x.  BS_EUNSUPPORTED as there, with the pieces of a row
+ * rounded up to a power of two, at most 64.
  */
 int bs_norm_rope(const bs_norm *norm, const bs_rope *rope, const bs_heads *x, const bs_heads *y, int32_t n_tensors, int32_t dtype, int32_t n_tokens,
                  int32_t head_dim, const int32_t *positions, int64_t axis_stride, void *stream);
@@ -538,7 +540,7 @@ int bs_norm_rope(const bs_norm *norm, const bs_rope *rope, const bs_heads *x, co
  *   dx           as many heads as x; may be x or dy (same data and strides), else it does not overlap them; rows of dx lie apart, those of x and dy may be
  *                the same one (stride 0)
  *   workspace    at least bs_norm_rope_grad_workspace bytes, 16-byte aligned; not looked at if dweight is NULL
- * Same inputs, same bits.
+ * Any number of tokens.  Same inputs, same bits.
  */
 int bs_norm_rope_grad(const bs_norm *norm, const bs_rope *rope, const bs_heads *x, const bs_heads *dy, const bs_heads *dx, float *dweight, int32_t n_tensors,
                       int32_t dtype, int32_t n_tokens, int32_t head_dim, const int32_t *positions, int64_t axis_stride, void *workspace, int64_t workspace_bytes,

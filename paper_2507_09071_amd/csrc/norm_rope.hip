@@ -437,7 +437,7 @@ int run_norm(NormArgs &p, const bs_norm &norm, const bs_rope *rope, int32_t dtyp
     // ahead (847 tokens of 40 + 8 + 8 heads into the cache: 11.2 -> 9.0 us).  Back, where a thread has three times the registers: an eighth of a million (5K tokens, 32 + 16
     // heads in fp32: 79 -> 77 us, and fewer parts to join).
     const int64_t items = (int64_t)a.n_tokens << p.lane_bits;
-    if (items > INT32_MAX) return BS_EUNSUPPORTED;
+    if (!gradient && items > INT32_MAX) return BS_EUNSUPPORTED;   // (norm_rows counts them in 32 bits, norm_grad_rows in 64)
     hipError_t err = hipSuccess;
     int splits[3] = {0, 0, 0};   // up to and with each job
     dim3 grid(0);
