@@ -352,8 +352,7 @@ extern "C" int bs_cache_append(const bs_cache *cache, const bs_heads *k, const b
 {
     using namespace bs;
     RopeArgs a{};
-    if (int rc = check_cache(cache)) return rc;
-    if (q && !rope) return BS_EINVAL;
     if (int rc = append_args(&a, cache, k, v, n_tokens, token_seq, token_slot, rope, positions, axis_stride, q, q_out, slots, token_order)) return rc;
+    if (q && !rope) return BS_EINVAL;
     return run_rope(a, rope, cache->dtype, cache->head_dim, false, (hipStream_t)stream);
 }
