@@ -305,6 +305,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Layout<T, D, NRB, WR, WK>::kPerCu * 
 {
     using TR = Layout<T, D, NRB, WR, WK>;
     constexpr bool BF16 = sizeof(T) == 2, SHARED = WR > 1;
+    static_assert(!(BF16 && SHARED), "bf16 waves that share their blocks are those of tree_wide");
     constexpr int KEYS = TR::kKeys, ROWB = TR::kRowBytes, BLK = TR::kBlock, NI = TR::kLoads, NI16 = TR::kLoads16, SUB = KEYS / 16, OWN = TR::kOwn;
     constexpr int ROWS = TR::kRows, NB = D / 16, CH4 = D / 4, WAVES = TR::kWaves, THREADS = TR::kThreads, KSTEPS = D * (int)sizeof(T) / 64;
     extern __shared__ __align__(1024) unsigned char lds[];
