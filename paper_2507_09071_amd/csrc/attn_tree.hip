@@ -10,9 +10,9 @@
 //    are joined by a second kernel in a fixed order;
 //  * masks cost nothing but at the end: slots below the length are seen by all, and only blocks that reach behind it (or hold the begin of a window, or a slot
 //    without a page) are masked, by 32 bits per row and block.  A window is laid on the words of a token's mask.
-// With d 128 in bf16, where a plain read reaches 6.2 TB/s, joins included: two sequences of 150K slots, 16 KV heads, 128 rows of each, 2.47 GB of K and V: 665 us; its
+// With d 128 in bf16, where a plain read reaches 6.2 TB/s, joins included: two sequences of 150K slots, 16 KV heads, 128 rows of each, 2.47 GB of K and V: 645 to 665 us; its
 // loads alone take 450, and what holds the rest back is power, of which the products of the probabilities' three numbers take their share (two numbers: 578).  One of
-// 39.5K slots, 4 KV heads, 182 rows, 81 MB that are walked twice: 49 us.  48 sequences of up to 16K slots, 8 KV heads, up to 80 rows, 504 MB, capped scores: 126 us.
+// 39.5K slots, 4 KV heads, 182 rows, 81 MB that are walked twice: 49 to 51 us.  48 sequences of up to 16K slots, 8 KV heads, up to 80 rows, 504 MB, capped scores: 126 to 131 us.
 #include "attn_common.h"
 #include "cache_attn.h"
 
@@ -121,8 +121,8 @@ __device__ inline Seq seq_of(const TreeArgs &a, int s, LOAD load)
     v.blocks = (v.n + L::kKeys - 1) / L::kKeys - v.first;
     v.groups = (v.T * a.G + L::kRows - 1) / L::kRows;
     v.items = v.groups * a.cache.n_kv_heads;
-    // groups of like size, in whole waves: a share is as long for few rows as for many (8 sequences of 4K to 16K slots, 140 rows: 75 -> 70 us; 39.5K slots, 182 rows:
-    // 47.6 -> 46.5)
+    // groups of like size, in whole waves: a share is as long for few rows as for many (39.5K slots, 182 rows: 49.6 -> 48.6 us; 8 sequences of 4K to
+    // 16K slots, 140 rows: 79 -> 78)
     v.rows = L::kRows;
     if (L::kEven > 0 && v.groups > 1) v.rows = ((v.T * a.G + v.groups - 1) / v.groups + L::kEven - 1) / L::kEven * L::kEven;
     v.units = v.T > 0 ? v.blocks + L::kItem : 0;
@@ -761,7 +761,8 @@ template <int D>
 struct Wide {
     static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves, kKeys = 32, kTurns = 1, kPerCu = 2;
     static constexpr int kEven = 32;                          // rows of a wave
-    static constexpr int kItem = 4;                           // (see Layout; 48 sequences of up to 80 rows with 2, 3, 4, 5, 6, 8: 151, 133, 127, 128, 128, 129 us)
+    static constexpr int kItem = 4;                           // (see Layout; 48 sequences of up to 80 rows with 2, 3, 4, 5, 6, 8: 151, 133, 127, 128, 128, 129 us; 16 of 40 rows at
+                                                              // d 64: 93, 93, 93, 92, 92, 92)
     static constexpr int kRowBytes = 2 * D, kBlock = kKeys * kRowBytes;                        // a block of K or V
     static constexpr int kLoads16 = 16 * kRowBytes / 1024;    // LDS-direct instructions per 16 slots, which lie in one page
     static constexpr int kSlots = D == 64 ? 8 : 4;            // blocks of K, of V, that the LDS holds
@@ -1219,7 +1220,7 @@ auto with_rows(int32_t M, bool cap, F f)
 }
 
 // The M that a sequence's rows per KV head are cut by.  Measured with all of them, in us, 32 query heads on 8; bf16: 16 sequences of 4K to 16K slots, fp32: 4
-// of 8K to 16K:
+// of 8K to 16K, over the logarithm:
 //              rows    bf16: 16     32     40     64    128  |  fp32: 16     32     64    128
 //     d 128, M = 16       113.6  187.9  268.9  353.3  683.9  |      80.7  132.5  244.5  482.0
 //            M = 32       119.2  120.0  189.6  193.7  370.1  |      96.2   99.6  175.7  332.4
